@@ -9,7 +9,8 @@ kv head of K and of V, a power of two.  K codes lie [page, kv head, head_dim / 1
   them within 448, and no less than the page's own where the run does not begin the page; codes that were there are rounded
   anew to a scale that has grown.
 * attention: every token of a mixed batch (decode tokens, prefill chunks, a finetune window) over its sequence's cached positions.
-* expand: pages written out in the type of the activations, as the window's backward pass and 16-bit pools have them.
+* expand: a sequence's pages written out in the type of the activations, as the window's backward pass and 16-bit pools have
+  them; slots behind its last token are zeros there.
 
 `own` false: `run` is that, in elementary operations; true: the package's calls.  Heads are those of the 8B, 14B / 32B and
 small fp32 configurations.  Lengths are a function of the case; values and physical pages come from the seed.
@@ -69,7 +70,7 @@ def listed():
         # a finetune sequence's pages for its backward pass
         dict(name="expand_8b_2048", op="expand", heads="8b", dtype="bf16", tokens=2048, spare=100),
         # a long sequence that moves to a pool in 16 bits
-        dict(name="expand_14b_32768", op="expand", heads="14b", dtype="bf16", tokens=32768, spare=100),
+        dict(name="expand_14b_32749", op="expand", heads="14b", dtype="bf16", tokens=32749, spare=100),
     ]
 
 
@@ -181,6 +182,7 @@ def _inputs(case, seed):
             codes[o:o + n] = c.view(n, nkv, d // 16, 16, PAGE).transpose(3, 4) if keys else c
             scale[o:o + n] = s
     if case["op"] == "expand":
+        st.tokens = case["tokens"]
         st.src = st.pages[0].to(torch.int32).cuda()
         st.dst = torch.randperm(counts[0], generator=order).to(torch.int32).cuda()
         st.out_k = torch.zeros((counts[0], nkv, PAGE, d), dtype=st.dtype, device="cuda")
@@ -331,9 +333,12 @@ def run(st):
         _store(st, x[:, nq + nkv:], st.v_codes, st.v_scale, False)
         return {"q": st.q_out, "k": st.k_codes.view(E4M3), "v": st.v_codes.view(E4M3), "k_scale": st.k_scale, "v_scale": st.v_scale}
     src, dst = st.src.long(), st.dst.long()
+    there = (torch.arange(len(src) * PAGE, device="cuda") < st.tokens).view(-1, 1, PAGE)
     x = st.k_codes[src].view(E4M3).float() * st.k_scale[src][:, :, None, None, None]
-    st.out_k[dst] = x.transpose(2, 3).reshape(len(src), st.nkv, PAGE, st.d).to(st.dtype)
-    st.out_v[dst] = (st.v_codes[src].view(E4M3).float() * st.v_scale[src][:, :, None, None]).to(st.dtype)
+    x = x.transpose(2, 3).reshape(len(src), st.nkv, PAGE, st.d)
+    st.out_k[dst] = torch.where(there[..., None], x, torch.zeros_like(x)).to(st.dtype)
+    x = st.v_codes[src].view(E4M3).float() * st.v_scale[src][:, :, None, None]
+    st.out_v[dst] = torch.where(there[:, :, None], x, torch.zeros_like(x)).to(st.dtype)
     return {"k": st.out_k, "v": st.out_v}
 
 
@@ -364,7 +369,7 @@ def _own_run(st):
     if st.op == "append":
         st.kv8.flexco_kv8_append(st.cfg, st.batch.maps, st.batch.runs, st.batch.n_runs, st.qkv, st.pool, st.q_out, st.nq * st.d)
         return {"q": st.q_out, "k": st.k_codes.view(E4M3), "v": st.v_codes.view(E4M3), "k_scale": st.k_scale, "v_scale": st.v_scale}
-    st.kv8.flexco_kv8_expand(st.cfg, st.pool, st.src, st.wide, st.dst, len(st.src))
+    st.kv8.flexco_kv8_expand(st.cfg, st.pool, st.src, st.tokens, st.wide, st.dst)
     return {"k": st.out_k, "v": st.out_v}
 
 
@@ -392,6 +397,7 @@ def exact(case, seed):
     st = _inputs(case, seed)
     if st.op == "expand":
         k, v = _cached64(st, 0, PAGE * len(st.pages[0]))
+        k[:, st.tokens:], v[:, st.tokens:] = 0.0, 0.0
         dst = st.dst.long()
         out_k = torch.empty(st.out_k.shape, dtype=torch.float64, device="cuda")
         out_v = torch.empty(st.out_v.shape, dtype=torch.float64, device="cuda")
