@@ -10,8 +10,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.environ.get("FLEXCO_BUILD_OBJ", os.path.join(ROOT, "_build"))
 LIB = os.environ.get("FLEXCO_BUILD_LIB", os.path.join(HERE, "libflexco.so"))
-SOURCES = ["flexco_maps.cpp", "flexco_sched.cpp", "flexco_prune.cpp", "flexco_api.hip", "kernels_generic.hip", "attn_generic.hip", "gemm_f32.hip", "gemm_mfma.hip",
-           "attn_mfma.hip", "attn_chunk_mfma.hip", "lora_mfma.hip", "attn_bwd_mfma.hip", "probes.hip", "train_head.hip", "relu_bitmask.hip"]
+SOURCES = ["flexco_maps.cpp", "flexco_sched.cpp", "flexco_prune.cpp", "flexco_kv8_host.cpp", "flexco_api.hip", "kernels_generic.hip", "attn_generic.hip", "gemm_f32.hip", "gemm_mfma.hip",
+           "attn_mfma.hip", "attn_chunk_mfma.hip", "lora_mfma.hip", "attn_bwd_mfma.hip", "probes.hip", "train_head.hip", "relu_bitmask.hip",
+           "kv8_cache.hip", "kv8_attn_generic.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-Wno-unused-command-line-argument",
@@ -56,11 +57,11 @@ def build(verbose=True):
     return LIB
 
 
-HOST_SOURCES = ["flexco_maps.cpp", "flexco_sched.cpp", "flexco_prune.cpp"]
+HOST_SOURCES = ["flexco_maps.cpp", "flexco_sched.cpp", "flexco_prune.cpp", "flexco_kv8_host.cpp"]
 
 
 def build_host_sanitized(out_path):
-    """The host-only sources (index maps, scheduler, graph pruning) as a library of their own, compiled for the CPU
+    """The host-only sources (index maps, scheduler, graph pruning, runs of the 8-bit cache) as a library of their own, compiled for the CPU
     with AddressSanitizer and UndefinedBehaviorSanitizer (any finding aborts).  Load it with the sanitizer runtime
     preloaded: LD_PRELOAD=$(g++ -print-file-name=libasan.so) FLEXCO_LIB_PATH=<out_path> FLEXCO_HOST_ONLY=1."""
     cxx = os.environ.get("CXX", "g++")

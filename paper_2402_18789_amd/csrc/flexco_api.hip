@@ -10,6 +10,7 @@
 
 #include "attn_plan.h"
 #include "flexco_internal.h"
+#include "kv8_internal.h"
 
 using namespace flexco;
 
@@ -392,11 +393,34 @@ int32_t check_maps(const flexco_layer_cfg& c, const flexco_maps* m) {
   return FLEXCO_OK;
 }
 
+int32_t check_kv8_pool(const flexco_layer_cfg& c, const flexco_kv8_pool* p) {
+  FLEXCO_CHECK(p != nullptr && p->k_codes && p->v_codes && p->k_scale && p->v_scale, FLEXCO_EINVAL, "8-bit kv pool is NULL");
+  FLEXCO_CHECK(aligned16(p->k_codes) && aligned16(p->v_codes), FLEXCO_EINVAL, "8-bit kv pool: codes are not 16-byte aligned");
+  FLEXCO_CHECK((((uintptr_t)p->k_scale | (uintptr_t)p->v_scale) & 3u) == 0, FLEXCO_EINVAL, "8-bit kv pool: scales are not 4-byte aligned");
+  FLEXCO_CHECK(p->num_pages > 0, FLEXCO_EINVAL, "8-bit kv pool has no pages");
+  FLEXCO_CHECK(p->page_size == c.page_size, FLEXCO_ESHAPE, "8-bit pool page_size %d != cfg page_size %d", p->page_size, c.page_size);
+  FLEXCO_CHECK(c.head_dim % 16 == 0, FLEXCO_ESHAPE, "an 8-bit cache takes head_dim in multiples of 16 (got %d)", c.head_dim);
+  return FLEXCO_OK;
+}
+
 // the page ids inside the maps were validated against a pool of m.num_pages pages: a smaller pool would be
 // read and written past its end
 int32_t check_maps_pool(const flexco_maps& m, const flexco_kv_pool& p) {
   FLEXCO_CHECK(m.num_pages <= p.num_pages, FLEXCO_EPAGE,
                "maps were built for a pool of %d pages, the pool given has %d", m.num_pages, p.num_pages);
+  return FLEXCO_OK;
+}
+int32_t check_maps_pool(const flexco_maps& m, const flexco_kv8_pool& p) {
+  FLEXCO_CHECK(m.num_pages <= p.num_pages, FLEXCO_EPAGE,
+               "maps were built for a pool of %d pages, the 8-bit pool given has %d", m.num_pages, p.num_pages);
+  return FLEXCO_OK;
+}
+
+// the runs of an append: one block per (run, kv head)
+int32_t check_runs(const flexco_layer_cfg& c, const flexco_maps& m, const int32_t* runs, int32_t n_runs) {
+  FLEXCO_CHECK(runs != nullptr && ((uintptr_t)runs & 3u) == 0, FLEXCO_EINVAL, "runs is NULL or misaligned");
+  FLEXCO_CHECK(n_runs > 0 && n_runs <= m.T, FLEXCO_EINVAL, "%d runs for a batch of %d tokens", n_runs, m.T);
+  FLEXCO_CHECK((int64_t)n_runs * c.n_kv_heads <= (1 << 24), FLEXCO_EUNSUPPORTED, "%d runs x %d heads are too many", n_runs, c.n_kv_heads);
   return FLEXCO_OK;
 }
 
@@ -750,6 +774,18 @@ int32_t run_attention(const flexco_layer_cfg& c, const flexco_maps& m, const voi
   return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, fold, keep);
 }
 
+// the same over an 8-bit pool
+int32_t run_kv8_attention(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
+                          void* out, size_t ldo, float* lse, float* part_ml, float* part_acc, hipStream_t s, const AttnKeep* keep = nullptr) {
+  {
+    KernelTimerScope ts(FLEXCO_K_GENERIC, s);
+    FLEXCO_TRY(launch_kv8_attention_generic(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep));
+  }
+  if (m.n_parts == m.n_tiles) return FLEXCO_OK;
+  KernelTimerScope ts(FLEXCO_K_ATTN_MERGE, s);
+  return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, 1, keep);
+}
+
 }  // namespace
 
 namespace flexco {
@@ -941,15 +977,28 @@ extern "C" int32_t flexco_lora_fwd_static(const void* x, void* y, int32_t T, int
                        seg_adapter, n_seg, u, stream);
 }
 
+// an 8-bit cache in the place of the 16-bit pool, with the batch's runs
+struct Kv8Cache {
+  const flexco_kv8_pool* pool;
+  const int32_t* runs;
+  int32_t n_runs;
+};
+
 static int32_t layer_forward_impl(const flexco_layer_cfg* cfg, const flexco_base_weights* w, const Adapters& ad,
                                   const flexco_maps* maps, const void* x_in, void* x_out, const flexco_kv_pool* pool,
                                   const flexco_ft_state* ft, void* ws, size_t ws_bytes, void* stream,
-                                  const flexco_ia3* ia3 = nullptr) {
+                                  const flexco_ia3* ia3 = nullptr, const Kv8Cache* kv8 = nullptr) {
   FLEXCO_TRY(check_cfg(cfg));
   FLEXCO_TRY(check_weights(w));
   FLEXCO_TRY(check_maps(*cfg, maps));
-  FLEXCO_TRY(check_pool(*cfg, pool));
-  FLEXCO_TRY(check_maps_pool(*maps, *pool));
+  if (kv8) {
+    FLEXCO_TRY(check_kv8_pool(*cfg, kv8->pool));
+    FLEXCO_TRY(check_maps_pool(*maps, *kv8->pool));
+    FLEXCO_TRY(check_runs(*cfg, *maps, kv8->runs, kv8->n_runs));
+  } else {
+    FLEXCO_TRY(check_pool(*cfg, pool));
+    FLEXCO_TRY(check_maps_pool(*maps, *pool));
+  }
   const flexco_layer_cfg& c = *cfg;
   const flexco_maps& m = *maps;
   if (ia3) {
@@ -1019,7 +1068,7 @@ static int32_t layer_forward_impl(const flexco_layer_cfg* cfg, const flexco_base
   {
     const int tg[3] = {FLEXCO_T_Q, FLEXCO_T_K, FLEXCO_T_V}, c0[3] = {0, qd, qd + kd};
     // (few tokens: the rotation adds the projection's partial sums; (IA)^3 scales the rows in between)
-    const bool sums_ok = dt == FLEXCO_BF16 && !ia3 && aligned16(w->bqkv) && rope_append_vec(c, k.qkv, *pool, ft ? ft->q_cache : nullptr);
+    const bool sums_ok = dt == FLEXCO_BF16 && !ia3 && !kv8 && aligned16(w->bqkv) && rope_append_vec(c, k.qkv, *pool, ft ? ft->q_cache : nullptr);
     FLEXCO_TRY(forward_projection(c, ad, m, k.h, H, w->wqkv, w->bqkv, nullptr, 0, k.qkv, qkvd, tg, c0, 3, k, ft, s, nullptr,
                                   sums_ok ? &qkv_sums : nullptr, within1 ? &norm1 : nullptr, x_in));
   }
@@ -1032,11 +1081,15 @@ static int32_t layer_forward_impl(const flexco_layer_cfg* cfg, const flexco_base
     sa.ft_tok0 = m.ft_tok0; sa.n_ft = ft ? m.n_ft : 0; sa.ft_pos0 = m.ft_pos0;
     EW(launch_ia3_scale_rows(k.qkv, qkvd, m.lora_tok, m.n_lora, sa, dt, s));
   }
-  EW(launch_rope_append(c, k.qkv, m.tok_pos, m.slot, *pool, T, m.ft_tok0, m.n_ft, m.ft_pos0,
-                        ft ? ft->q_cache : nullptr, s, &qkv_sums, w->bqkv));
+  if (kv8)
+    EW(launch_kv8_append(c, m, kv8->runs, kv8->n_runs, k.qkv, *kv8->pool, k.qkv, qkvd, ft ? boff(ft->q_cache, p0 * qd, e) : nullptr, s));
+  else
+    EW(launch_rope_append(c, k.qkv, m.tok_pos, m.slot, *pool, T, m.ft_tok0, m.n_ft, m.ft_pos0,
+                          ft ? ft->q_cache : nullptr, s, &qkv_sums, w->bqkv));
   const AttnKeep keep{ft ? (void*)boff(ft->saved_attn, p0 * qd, e) : nullptr, ft ? ft->lse + p0 * c.n_q_heads : nullptr,
                       m.ft_tok0, ft ? m.n_ft : 0};
-  FLEXCO_TRY(run_attention(c, m, k.qkv, qkvd, *pool, k.attn, qd, nullptr, k.part_ml, k.part_acc, s, &keep));
+  if (kv8) FLEXCO_TRY(run_kv8_attention(c, m, k.qkv, qkvd, *kv8->pool, k.attn, qd, nullptr, k.part_ml, k.part_acc, s, &keep));
+  else FLEXCO_TRY(run_attention(c, m, k.qkv, qkvd, *pool, k.attn, qd, nullptr, k.part_ml, k.part_acc, s, &keep));
   {
     const int tg[1] = {FLEXCO_T_O}, c0[1] = {0};
     // (its partial sums and the residual are added by the norm that reads it next)
@@ -1464,3 +1517,71 @@ extern "C" int32_t flexco_model_backward(const flexco_layer_cfg* cfg, const flex
   return FLEXCO_OK;
 }
 
+
+// ---- the 8-bit cache (flexco_kv8.h) ---------------------------------------------------------------------
+extern "C" int32_t flexco_kv8_append(const flexco_layer_cfg* cfg, const flexco_maps* maps, const int32_t* runs, int32_t n_runs,
+                                     const void* qkv, const flexco_kv8_pool* pool, void* q_out, size_t ld_q, void* stream) {
+  clear_error();
+  FLEXCO_TRY(check_cfg(cfg));
+  FLEXCO_TRY(check_maps(*cfg, maps));
+  FLEXCO_TRY(check_kv8_pool(*cfg, pool));
+  FLEXCO_TRY(check_maps_pool(*maps, *pool));
+  FLEXCO_TRY(check_runs(*cfg, *maps, runs, n_runs));
+  FLEXCO_CHECK(qkv && q_out, FLEXCO_EINVAL, "qkv or q_out is NULL");
+  FLEXCO_CHECK(aligned16(qkv) && aligned16(q_out), FLEXCO_EINVAL, "misaligned pointer");
+  const size_t e = esize(cfg->dtype), qd = (size_t)cfg->n_q_heads * cfg->head_dim;
+  const size_t qkvd = qd + 2 * (size_t)cfg->n_kv_heads * cfg->head_dim;
+  FLEXCO_CHECK(ld_q >= qd && ld_q * e % 16 == 0, FLEXCO_ESHAPE, "ld_q %zu: at least %zu, rows a multiple of 16 bytes apart", ld_q, qd);
+  const char *in0 = (const char*)qkv, *in1 = in0 + (size_t)maps->T * qkvd * e, *o0 = (const char*)q_out;
+  const char* o1 = o0 + ((size_t)(maps->T - 1) * ld_q + qd) * e;
+  FLEXCO_CHECK((q_out == qkv && ld_q == qkvd) || o1 <= in0 || in1 <= o0, FLEXCO_EINVAL,
+               "q_out overlaps qkv and is not its query columns in place");
+  hipStream_t s = (hipStream_t)stream;
+  EW(launch_kv8_append(*cfg, *maps, runs, n_runs, qkv, *pool, q_out, ld_q, nullptr, s));
+  return FLEXCO_OK;
+}
+
+extern "C" int32_t flexco_kv8_attention(const flexco_layer_cfg* cfg, const flexco_maps* maps, const void* q,
+                                        const flexco_kv8_pool* pool, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  FLEXCO_TRY(check_cfg(cfg));
+  FLEXCO_TRY(check_maps(*cfg, maps));
+  FLEXCO_TRY(check_kv8_pool(*cfg, pool));
+  FLEXCO_TRY(check_maps_pool(*maps, *pool));
+  FLEXCO_CHECK(q && out && ws, FLEXCO_EINVAL, "q, out or ws is NULL");
+  FLEXCO_CHECK(aligned16(q) && aligned16(out) && aligned16(ws) && aligned16(lse), FLEXCO_EINVAL, "misaligned pointer");
+  const size_t prow = (size_t)maps->n_parts * cfg->n_kv_heads * cols_per_tile(*cfg);
+  const size_t ml_bytes = align_up(sizeof(float) * prow * 2, 256);
+  const size_t need = ml_bytes + sizeof(float) * prow * cfg->head_dim;
+  FLEXCO_CHECK(need <= ws_bytes, FLEXCO_EWORKSPACE, "attention needs %zu workspace bytes, got %zu", need, ws_bytes);
+  const size_t qd = (size_t)cfg->n_q_heads * cfg->head_dim;
+  return run_kv8_attention(*cfg, *maps, q, qd, *pool, out, qd, lse, (float*)ws, (float*)((char*)ws + ml_bytes), (hipStream_t)stream);
+}
+
+extern "C" int32_t flexco_kv8_expand(const flexco_layer_cfg* cfg, const flexco_kv8_pool* pool, const int32_t* src_pages,
+                                     int32_t n_tokens, const flexco_kv_pool* wide, const int32_t* dst_pages, void* stream) {
+  clear_error();
+  FLEXCO_TRY(check_cfg(cfg));
+  FLEXCO_TRY(check_kv8_pool(*cfg, pool));
+  FLEXCO_TRY(check_pool(*cfg, wide));
+  FLEXCO_CHECK(n_tokens >= 0 && n_tokens < (1 << 30), FLEXCO_EINVAL, "n_tokens %d outside [0, 2^30)", n_tokens);
+  if (n_tokens == 0) return FLEXCO_OK;
+  FLEXCO_CHECK(src_pages && dst_pages, FLEXCO_EINVAL, "a page list is NULL");
+  FLEXCO_CHECK((((uintptr_t)src_pages | (uintptr_t)dst_pages) & 3u) == 0, FLEXCO_EINVAL, "a page list is misaligned");
+  const int64_t n_pages = ((int64_t)n_tokens + cfg->page_size - 1) / cfg->page_size;
+  FLEXCO_CHECK(n_pages * cfg->n_kv_heads <= (1 << 24), FLEXCO_EUNSUPPORTED, "%lld pages x %d heads are too many for one call",
+               (long long)n_pages, cfg->n_kv_heads);
+  hipStream_t s = (hipStream_t)stream;
+  EW(launch_kv8_expand(*cfg, *pool, src_pages, n_tokens, *wide, dst_pages, s));
+  return FLEXCO_OK;
+}
+
+extern "C" int32_t flexco_kv8_layer_forward(const flexco_layer_cfg* cfg, const flexco_base_weights* w, const flexco_lora* lora,
+                                            const flexco_maps* maps, const int32_t* runs, int32_t n_runs, const void* x_in, void* x_out,
+                                            const flexco_kv8_pool* pool, const flexco_ft_state* ft, void* ws, size_t ws_bytes,
+                                            void* stream) {
+  clear_error();
+  const Adapters ad{lora, lora ? 1 : 0, true};
+  const Kv8Cache kv8{pool, runs, n_runs};
+  return layer_forward_impl(cfg, w, ad, maps, x_in, x_out, nullptr, ft, ws, ws_bytes, stream, nullptr, &kv8);
+}

@@ -12,6 +12,7 @@
 #include <vector>
 #include "flexco_internal.h"
 #include "device_types.h"
+#include "rope.h"
 
 namespace flexco {
 
@@ -400,21 +401,6 @@ __global__ __launch_bounds__(1024) void rmsnorm_bwd_wide_kernel(const bf16_t* __
       st4(dx + row * H + i, o);
     }
   }
-}
-
-// Rotation angles.  Pair i of a head turns by pos * theta^(-2 i / d).  The host hands over the frequencies in
-// revolutions, theta^(-2 i / d) / (2 pi), as doubles (a kernel argument: pow and a double-precision sincos per
-// (token, i) on the device were a third of these kernels' run time).  The device takes the fractional part of
-// pos * rev in double precision (exact to 1e-10 of a turn at any position) and the sine and cosine of that
-// fraction of a turn in single precision (angle in [0, 2 pi): about 5e-7 absolute).
-constexpr int ROPE_MAX_HALF = 128;   // head_dim <= 256
-struct RopeFreq {
-  double rev[ROPE_MAX_HALF];
-};
-__device__ inline void rope_cos_sin(const RopeFreq& f, int i, int pos, float* c, float* sn) {
-  const double r = (double)pos * f.rev[i];
-  const float turn = (float)(r - floor(r));
-  sincosf(turn * 6.283185307179586f, sn, c);
 }
 
 // --------------------------------------------------------------------------------------
@@ -1353,7 +1339,7 @@ int32_t launch_rmsnorm_bwd(const void* x, const void* g, const void* dh, const v
 }
 
 // The frequencies of a (theta, head_dim) pair, computed once (a model has one pair; a lock guards the few cached ones).
-static int32_t rope_freq(const flexco_layer_cfg& c, RopeFreq* out) {
+int32_t rope_freq(const flexco_layer_cfg& c, RopeFreq* out) {
   const int half = c.head_dim / 2;
   if (half > ROPE_MAX_HALF) return fail(FLEXCO_EUNSUPPORTED, "rotary embedding: head_dim %d above %d", c.head_dim, 2 * ROPE_MAX_HALF);
   struct Entry { float theta; int d; RopeFreq f; };

@@ -1,0 +1,18 @@
+// Launchers of the 8-bit cache's kernels (no validation, the entry points have done it).
+#pragma once
+#include "flexco_internal.h"
+#include "flexco_kv8.h"
+
+namespace flexco {
+
+// q_cache: NULL, or where the finetune window's rotated queries go as well (its first row's)
+int32_t launch_kv8_append(const flexco_layer_cfg& c, const flexco_maps& m, const int32_t* runs, int n_runs, const void* qkv,
+                          const flexco_kv8_pool& pool, void* q_out, size_t ld_q, void* q_cache, hipStream_t s);
+int32_t launch_kv8_expand(const flexco_layer_cfg& c, const flexco_kv8_pool& pool, const int32_t* src, int n_tokens,
+                          const flexco_kv_pool& wide, const int32_t* dst, hipStream_t s);
+// partial rows as the 16-bit kernels leave them (attn_generic.hip), for launch_attention_merge
+int32_t launch_kv8_attention_generic(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq,
+                                     const flexco_kv8_pool& pool, float* part_ml, float* part_acc, void* out, size_t ldo, float* lse,
+                                     hipStream_t s, const AttnKeep* keep);
+
+}  // namespace flexco
