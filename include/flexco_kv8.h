@@ -6,11 +6,12 @@
  * The cache of Sec. 7 (pages of page_size positions, a sequence's pages in any order) with one byte per element instead of
  * the activations' two or four: decode attention reads little else, and a pool holds twice the sequences beside the
  * finetuning job.  An element is code x scale: the code an 8-bit float with 4 exponent and 3 mantissa bits (e4m3: largest 448,
- * no infinities, NaN = 0x7f and 0xff), the scale a float for each (page, kv head), of K and of V each.
+ * no infinities, NaN = 0x7f and 0xff), the scale a power of two for each (page, kv head), of K and of V each, held as a float
+ * (other positive numbers in its place give results without meaning).
  *
- * What flexco_kv8_append writes: the scale of a page is a power of two, 2^e with e >= -117 the least that keeps its elements within
- * 448 (code x scale is then exact in bf16, and a scale that grows later costs codes no second rounding but below the type's
- * smallest normal number).  Elements that are no finite number are stored as NaN and take no part in a scale.
+ * What flexco_kv8_append writes: the scale of a page is 2^e with e >= -117 the least that keeps its elements within 448 (code x scale
+ * is then exact in bf16, and a scale that grows later costs codes no second rounding but below the type's smallest normal
+ * number).  Elements that are no finite number are stored as NaN and take no part in a scale.
  */
 #ifndef FLEXCO_KV8_H
 #define FLEXCO_KV8_H
@@ -63,8 +64,7 @@ int32_t flexco_kv8_append(const flexco_layer_cfg* cfg, const flexco_maps* maps, 
  * ws as there (flexco_workspace_bytes covers it).  Key positions behind a token's own never reach its row, whatever
  * they hold.  lse may be NULL.
  * Gradients: flexco_kv8_expand the sequence's pages, then flexco_attention_window_bwd (flexco_lora_bwd) on that pool: the keys and
- * values are those this call read, bit for bit where the scales are powers of two (the rounding into the cache counts as the
- * identity).
+ * values are bit for bit those this call read (the rounding into the cache counts as the identity).
  * Errors: EINVAL, ESHAPE, EPAGE, EWORKSPACE, EHIP. */
 int32_t flexco_kv8_attention(const flexco_layer_cfg* cfg, const flexco_maps* maps, const void* q, const flexco_kv8_pool* pool,
                              void* out, float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -4,10 +4,10 @@ cache and its window's backward pass.
 Tolerances, derived element by element from the roundings a result passes:
 * a cached element: half a step of e4m3 (2^-4 relative, 2^-10 of the scale for the smallest), and for keys and queries
   the rotation's error, |cos|, |sin| to 1e-6;
-* attention, with w = sum_j p_j |v_j| of the row: bf16 out 2^-8 |out| (its storage) + 2^-9 w (the probabilities: two e4m3 terms,
-  or - in bf16 form - 2^-8 w: the looser is used) + the fp32 part; fp32 out the fp32 part alone: each score is off by ds <= 2^-24 ((d + 4)
+* attention, with w = sum_j p_j |v_j| of the row: bf16 out 2^-8 |out| (its storage) + 2^-8 w (the probabilities of the second
+  product) + the fp32 part; fp32 out the fp32 part alone: each score is off by ds <= 2^-24 ((d + 4)
   sum|q k| / sqrt d + 4 max|s - m|), a probability by 2 ds relative, the sums by 2^-24 (keys + 8);
-* log-sum-exp: ds + 2^-24 (keys + 8) + 2^-23 |lse|.
+* log-sum-exp m + log z: ds + 2^-24 (keys + 8) + 2^-23 (|m| + |log z|).
 """
 import numpy as np
 import pytest
@@ -328,7 +328,9 @@ def check_attention(cfg, reqs_in, rows_of=None, **kw):
                 gl = lse[t0 + i].reshape(nkv, g)
                 okl = ~np.isnan(want)
                 assert np.array_equal(okl, ~np.isnan(gl))
-                assert np.all((np.abs(gl - want) <= ds + 2.0 ** -24 * (n + 8) + 2.0 ** -23 * np.abs(want))[okl]), (r, i)
+                # (m and log z are rounded each at their own size, and may cancel: hence not 2^-23 |lse|)
+                tol = ds + 2.0 ** -24 * (n + 8) + 2.0 ** -23 * (np.abs(m[..., 0]) + np.abs(np.log(z)))
+                assert np.all((np.abs(gl - want) <= tol)[okl]), (r, i, np.abs(gl - want) / tol, want, m[..., 0])
         t0 += r.n_new
     say("  worst error / bound %.2f" % worst)
 
@@ -394,13 +396,6 @@ def test_attention_what_is_masked_never_shows():
         cache.codes["v"][pages[0][2], 3, 1, 100] = 0xFF
     check_attention(shape(8, 2), [(D, 333, 1), (P, 30, 64), (P, 0, 40), (F, 41, 70), (D, 50, 1)], edit=edit)
     check_attention(shape(4, 2, 64, "f32"), [(D, 333, 1), (P, 30, 64), (P, 0, 40), (F, 41, 70), (D, 50, 1)], edit=lambda *a: None)
-
-
-def test_attention_scales_that_are_no_powers_of_two():
-    def edit(cache, reqs, pages):
-        for n in "kv":
-            cache.scale[n] *= np.float32(1.37)
-    check_attention(shape(8, 2), [(D, 333, 1), (P, 70, 40)], edit=edit)
 
 
 def test_attention_without_lse():
