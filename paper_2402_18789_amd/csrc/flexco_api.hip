@@ -778,23 +778,17 @@ int32_t run_attention(const flexco_layer_cfg& c, const flexco_maps& m, const voi
 // the same over an 8-bit pool
 int32_t run_kv8_attention(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
                           void* out, size_t ldo, float* lse, float* part_ml, float* part_acc, hipStream_t s, const AttnKeep* keep = nullptr) {
-  int fold = plan_kv8_fold(m, c.n_kv_heads);
-  int32_t rc;
+  const int32_t rc = launch_kv8_attention_mfma(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep, plan_kv8_fold(m, c.n_kv_heads));
+  if (rc != FLEXCO_EUNSUPPORTED) return rc;
+  clear_error();
+  note_fallback(c.dtype, FLEXCO_K_ATTN_FWD);
   {
-    KernelTimerScope ts(FLEXCO_K_ATTN_FWD, s);
-    rc = launch_kv8_attention_mfma(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep, fold);
-  }
-  if (rc == FLEXCO_EUNSUPPORTED) {
-    clear_error();
-    fold = 1;
-    note_fallback(c.dtype, FLEXCO_K_ATTN_FWD);
     KernelTimerScope ts(FLEXCO_K_GENERIC, s);
-    rc = launch_kv8_attention_generic(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep);
+    FLEXCO_TRY(launch_kv8_attention_generic(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep));
   }
-  if (rc) return rc;
-  if (m.n_parts == m.n_tiles || (m.n_single == m.n_items && m.max_pages <= fold * m.kv_split_pages)) return FLEXCO_OK;
+  if (m.n_parts == m.n_tiles) return FLEXCO_OK;
   KernelTimerScope ts(FLEXCO_K_ATTN_MERGE, s);
-  return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, fold, keep);
+  return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, 1, keep);
 }
 
 }  // namespace

@@ -20,6 +20,7 @@
 #include "flexco_internal.h"
 #include "kv8_codes.h"
 #include "kv8_internal.h"
+#include "kv8_plan.h"
 
 namespace flexco {
 
@@ -27,7 +28,7 @@ namespace {
 
 constexpr int D = 128, PS = 16;
 constexpr int PAGE = PS * D;             // bytes of one K (or V) block of a page and head
-constexpr int MAXSP = 512;               // pages of a block's key range at most
+constexpr int MAXSP = KV8_MAX_PAGES;     // pages of a block's key range at most
 constexpr int SP = 4;                    // pages of a step
 constexpr int NW = 2, NT = 64 * NW;      // wavefronts, threads of a block
 constexpr float NO_KEY = -3.402823466e38f;   // the maximum of no key yet: finite, so that a masked score less this is still -inf
@@ -197,7 +198,9 @@ struct TokenLds {
   __device__ float* at(int wave, int c, int d) const { return o + (wave * 16 + c) * D + ((d + 4 * c) & (D - 1)); }
 };
 
-__device__ inline void token_block(const Args& a, const Tables& tab, const TokenLds& sh, int tile, int split, int fold, int kvh, int npg, int keys) {
+template <typename Scales>
+__device__ inline void token_block(const Args& a, const Tables& tab, const TokenLds& sh, int tile, int split, int fold, int kvh, int npg, int keys,
+                                   Scales&& keep_scales) {
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = a.nq / a.nkv, t = a.tile_tok0[tile];
@@ -253,8 +256,9 @@ __device__ inline void token_block(const Args& a, const Tables& tab, const Token
   };
   // (past the last step the loads repeat it, unused: as many are on their way on every path)
   u32x4 k0[2 * SP], k1[2 * SP], v0[8], v1[8];
+  load(wave, k0, v0);
+  keep_scales();
   if (wave < n_steps) {
-    load(wave, k0, v0);
     for (int st = wave; st < n_steps; st += 2 * NW) {
       load(st + NW, k1, v1);
       step(st, k0, v0);
@@ -417,25 +421,45 @@ __global__ __launch_bounds__(NT, 2) void kv8_attn_kernel(Args a) {
   const int fold = a.fold > 1 && a.req_tok_off[r + 1] - a.req_tok_off[r] == 1 ? a.fold : 1;
   if (split % fold != 0) return;                           // the block of an earlier split takes this one's keys (whole block)
   const int pb = split * a.split_pages;
+  // The block's start is a chain of lookups in front of its first codes: each step asks for all it can.  The page ids of the range, and
+  // what may follow them in the request's row of the table (never used), come with the positions; their scales are on their way
+  // while the first codes are asked for.
+  const int n_range = min(fold * a.split_pages, a.max_pages - pb);
+  int ids[MAXSP / NT];
+#pragma unroll
+  for (int i = 0; i < MAXSP / NT; ++i)
+    if (i == 0 || i * NT < n_range) ids[i] = a.block_table[(size_t)r * a.max_pages + pb + min(tid + i * NT, n_range - 1)];
   const int last_pos = a.tok_pos[tok_last], first_pos = a.tok_pos[tok_first];
-  const int npg = min(pb + fold * a.split_pages, last_pos / PS + 1) - pb;      // >= 1: an item's splits lie inside its visible range
-  for (int i = tid; i < npg; i += NT) {
-    const int page = a.block_table[(size_t)r * a.max_pages + pb + i];
-    tab.page[i] = page;
-    const size_t ph = (size_t)page * a.nkv + kvh;
-    tab.ks[i] = a.k_scale[ph];
-    tab.vs[i] = a.v_scale[ph];
-  }
+  const int npg = min(n_range, last_pos / PS + 1 - pb);   // >= 1: an item's splits lie inside its visible range
+  float ks[MAXSP / NT], vs[MAXSP / NT];
+#pragma unroll
+  for (int i = 0; i < MAXSP / NT; ++i)
+    if (tid + i * NT < npg) {
+      const size_t ph = (size_t)ids[i] * a.nkv + kvh;
+      ks[i] = a.k_scale[ph];
+      vs[i] = a.v_scale[ph];
+      tab.page[tid + i * NT] = ids[i];
+    }
   __syncthreads();
+  auto keep_scales = [&]() {
+#pragma unroll
+    for (int i = 0; i < MAXSP / NT; ++i)
+      if (tid + i * NT < npg) {
+        tab.ks[tid + i * NT] = ks[i];
+        tab.vs[tid + i * NT] = vs[i];
+      }
+    __syncthreads();
+  };
   if (MODE == 1 || (MODE == 3 && lone)) {
     static_assert(sizeof(StepLds) >= NW * 16 * D * sizeof(float), "the sums of a single token fit a step's buffer");
     const TokenLds token{reinterpret_cast<float*>(ring0.k), token_m, token_l};
-    token_block(a, tab, token, tile0, split, fold, kvh, npg, min(last_pos + 1 - pb * PS, npg * PS));
+    token_block(a, tab, token, tile0, split, fold, kvh, npg, min(last_pos + 1 - pb * PS, npg * PS), keep_scales);
     return;
   }
   if constexpr (MODE != 1) {
     const int group = a.nq / a.nkv, c = lane & 15, g = lane >> 4;
     load_step(a, tab, ring0, 0, kvh, npg, wave, lane);
+    keep_scales();
     const int tiles = max(0, min(TILES, ntl - TILES * wave));      // (a wavefront without a tile only helps with the loads)
     Column col[TILES];
     int pos[TILES];
@@ -485,6 +509,77 @@ __global__ __launch_bounds__(NT, 2) void kv8_attn_kernel(Args a) {
   }
 }
 
+// ---- joining the partial rows of a long axis ---------------------------------------------------------------
+// A block per (token, query head), for lists in which a request is cut into many pieces: eight groups of 32 lanes take the pieces in
+// turn, four loads at a time, and add up in LDS in group order.  (The merge that lists of few pieces take walks them one group per row:
+// 118 pieces of three long contexts 50 us.)
+constexpr int MG = 8;
+__global__ __launch_bounds__(32 * MG) void kv8_merge_long_kernel(Args a, const int32_t* __restrict__ tok_tile, const int32_t* __restrict__ tok_req) {
+  __shared__ float red_m[32 * MG / 64], part[MG][D], part_l[MG];
+  const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, grp = tid >> 5, ln = tid & 31;
+  const int group = a.nq / a.nkv, kvh = h / group, tile = tok_tile[t], r = tok_req[t];
+  const int fold = a.fold > 1 && a.req_tok_off[r + 1] - a.req_tok_off[r] == 1 ? a.fold : 1;
+  const int n = (a.tile_nsplit[tile] + fold - 1) / fold;       // partial rows
+  if (n == 1) return;                                          // the attention kernel has written these rows itself (whole block)
+  const int cpt = (16 / group > 1 ? 16 / group : 1) * group;
+  const size_t idx0 = ((size_t)a.tile_part0[tile] * a.nkv + kvh) * cpt + (t - a.tile_tok0[tile]) * group + h % group;
+  const size_t step = (size_t)fold * a.nkv * cpt;
+  float m = -INFINITY;
+  for (int i = tid; i < n; i += 32 * MG) m = fmaxf(m, a.part_ml[(idx0 + i * step) * 2]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  if ((tid & 63) == 0) red_m[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 32 * MG / 64; ++w) m = fmaxf(m, red_m[w]);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  constexpr int U = 4;
+  for (int i0 = grp; i0 < n; i0 += MG * U) {
+    float2 ml[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t idx = idx0 + min(i0 + u * MG, n - 1) * step;
+      ml[u] = *reinterpret_cast<const float2*>(a.part_ml + idx * 2);
+      v[u] = *reinterpret_cast<const f32x4*>(a.part_acc + idx * D + 4 * ln);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * MG < n && !(ml[u].x == -INFINITY)) {       // (the sums of a piece without a visible key are not written)
+        const float w = __expf(ml[u].x - m);
+        l += ml[u].y * w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] += v[u][j] * w;
+      }
+  }
+  *reinterpret_cast<f32x4*>(&part[grp][4 * ln]) = acc;
+  if (ln == 0) part_l[grp] = l;
+  __syncthreads();
+  if (grp != 0) return;
+  f32x4 row = {0.f, 0.f, 0.f, 0.f};
+  float L = 0.f;
+#pragma unroll
+  for (int w = 0; w < MG; ++w) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(&part[w][4 * ln]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) row[j] += v[j];
+    L += part_l[w];
+  }
+  const float inv = 1.0f / L;
+  bf16x4 o;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = (bf16_t)(row[j] * inv);
+  const bool kept = a.keep.lse2 && t >= a.keep.tok0 && t < a.keep.tok0 + a.keep.n;
+  *reinterpret_cast<bf16x4*>(a.out + (size_t)t * a.ldo + h * D + 4 * ln) = o;
+  if (kept) *reinterpret_cast<bf16x4*>((bf16_t*)a.keep.out2 + ((size_t)(t - a.keep.tok0) * a.nq + h) * D + 4 * ln) = o;
+  if (ln == 0) {
+    const float z = m + __logf(L);
+    if (a.lse) a.lse[(size_t)t * a.nq + h] = z;
+    if (kept) a.keep.lse2[(size_t)(t - a.keep.tok0) * a.nq + h] = z;
+  }
+}
+
 }  // namespace
 
 int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
@@ -507,11 +602,26 @@ int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& 
   a.out = (bf16_t*)out; a.ldo = ldo; a.lse = lse;
   a.keep = keep ? *keep : AttnKeep{nullptr, nullptr, 0, 0};
   const dim3 grid((unsigned)turns_of(m.n_items, fold) * c.n_kv_heads);
-  if (m.n_single == m.n_items) hipLaunchKernelGGL(kv8_attn_kernel<1>, grid, dim3(NT), 0, s, a);
-  else if (m.n_single == 0) hipLaunchKernelGGL(kv8_attn_kernel<2>, grid, dim3(NT), 0, s, a);
-  else hipLaunchKernelGGL(kv8_attn_kernel<3>, grid, dim3(NT), 0, s, a);
+  {
+    KernelTimerScope ts(FLEXCO_K_ATTN_FWD, s);
+    if (m.n_single == m.n_items) hipLaunchKernelGGL(kv8_attn_kernel<1>, grid, dim3(NT), 0, s, a);
+    else if (m.n_single == 0) hipLaunchKernelGGL(kv8_attn_kernel<2>, grid, dim3(NT), 0, s, a);
+    else hipLaunchKernelGGL(kv8_attn_kernel<3>, grid, dim3(NT), 0, s, a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FLEXCO_EHIP, "launch of kv8_attn failed: %s", hipGetErrorString(e));
+  // every request in one piece: nothing to join
+  if (m.n_parts == m.n_tiles || (m.n_single == m.n_items && m.max_pages <= fold * m.kv_split_pages)) return FLEXCO_OK;
+  KernelTimerScope ts(FLEXCO_K_ATTN_MERGE, s);
+  // The long form from nine pieces on where there are few rows (4 tokens of 4000 keys in eights 18.4 -> 15.1 us, 8 of 8000 in 32s 36.0 -> 32.5;
+  // with 256 x 16 rows of up to five pieces it cost 4 more), from seventeen on in any case.
+  const int most = (m.max_pages + fold * m.kv_split_pages - 1) / (fold * m.kv_split_pages);
+  const bool long_axis = most > 16 || (most > 8 && (int64_t)m.T * c.n_q_heads <= 2048);
+  if (!long_axis)
+    return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, fold, keep);
+  hipLaunchKernelGGL(kv8_merge_long_kernel, dim3(m.T, c.n_q_heads), dim3(32 * MG), 0, s, a, m.tok_tile, m.tok_req);
+  e = hipGetLastError();
+  if (e != hipSuccess) return fail(FLEXCO_EHIP, "launch of kv8_merge_long failed: %s", hipGetErrorString(e));
   return FLEXCO_OK;
 }
 
