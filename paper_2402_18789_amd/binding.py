@@ -207,7 +207,9 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        import torch
+        # (the handle torch.cuda.current_stream().cuda_stream wraps, 2.8 us of a call's 7)
+        if torch.cuda.is_initialized():
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
