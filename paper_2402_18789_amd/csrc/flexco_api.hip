@@ -11,7 +11,6 @@
 #include "attn_plan.h"
 #include "flexco_internal.h"
 #include "kv8_internal.h"
-#include "kv8_plan.h"
 
 using namespace flexco;
 
@@ -778,7 +777,7 @@ int32_t run_attention(const flexco_layer_cfg& c, const flexco_maps& m, const voi
 // the same over an 8-bit pool
 int32_t run_kv8_attention(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
                           void* out, size_t ldo, float* lse, float* part_ml, float* part_acc, hipStream_t s, const AttnKeep* keep = nullptr) {
-  const int32_t rc = launch_kv8_attention_mfma(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep, plan_kv8_fold(m, c.n_kv_heads));
+  const int32_t rc = launch_kv8_attention_mfma(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep);
   if (rc != FLEXCO_EUNSUPPORTED) return rc;
   clear_error();
   note_fallback(c.dtype, FLEXCO_K_ATTN_FWD);

@@ -30,7 +30,7 @@ constexpr int D = 128, PS = 16;
 constexpr int PAGE = PS * D;             // bytes of one K (or V) block of a page and head
 constexpr int MAXSP = KV8_MAX_PAGES;     // pages of a block's key range at most
 constexpr int SP = 4;                    // pages of a step
-constexpr int NW = 2, NT = 64 * NW;      // wavefronts, threads of a block
+constexpr int CHUNK_NW = 2;              // wavefronts of a chunk's block
 constexpr float NO_KEY = -3.402823466e38f;   // the maximum of no key yet: finite, so that a masked score less this is still -inf
 constexpr float LAG = 8.f;               // how far (log2) a column's maximum may run ahead of its reference point
 #define FLEXCO_GP(p) ((const __attribute__((address_space(1))) void*)(p))
@@ -192,13 +192,13 @@ struct Tables {
 // add up in LDS at the end: no barrier holds the stream.  Sixteen columns are one product's width; a token has as many as its
 // group has heads, and the matrix cores time to spare.
 struct TokenLds {
-  float* o;                // sums [NW][16][D]
+  float* o;                // sums [wavefronts][16][D]
   float (*m)[16], (*l)[16];
   // four channels of a column (turned from column to column, so that sixteen of them written at once lie in all banks)
   __device__ float* at(int wave, int c, int d) const { return o + (wave * 16 + c) * D + ((d + 4 * c) & (D - 1)); }
 };
 
-template <typename Scales>
+template <int NW, typename Scales>
 __device__ inline void token_block(const Args& a, const Tables& tab, const TokenLds& sh, int tile, int split, int fold, int kvh, int npg, int keys,
                                    Scales&& keep_scales) {
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
@@ -275,7 +275,7 @@ __device__ inline void token_block(const Args& a, const Tables& tab, const Token
   __syncthreads();
   // 32 threads per column
   const int dd = (tid & 31) * 4;
-  for (int cc = tid >> 5; cc < group; cc += NT / 32) {
+  for (int cc = tid >> 5; cc < group; cc += 2 * NW) {
     float M = sh.m[0][cc];
 #pragma unroll
     for (int w = 1; w < NW; ++w) M = fmaxf(M, sh.m[w][cc]);
@@ -303,8 +303,8 @@ struct StepLds {
 
 __device__ inline void load_step(const Args& a, const Tables& tab, StepLds& to, int st, int kvh, int npg, int wave, int lane) {
 #pragma unroll
-  for (int x = 0; x < SP / NW; ++x) {
-    const int n = NW * x + wave;                                                    // this wavefront's page
+  for (int x = 0; x < SP / CHUNK_NW; ++x) {
+    const int n = CHUNK_NW * x + wave;                                                    // this wavefront's page
     const size_t page = (size_t)__builtin_amdgcn_readfirstlane(tab.page[min(SP * st + n, npg - 1)]);
     const uint8_t* kb = a.k_codes + (page * a.nkv + kvh) * (size_t)PAGE + lane * 16;
     const uint8_t* vb = a.v_codes + (page * a.nkv + kvh) * (size_t)PAGE + lane * 16;
@@ -316,7 +316,7 @@ __device__ inline void load_step(const Args& a, const Tables& tab, StepLds& to, 
   }
 }
 
-constexpr int TILES = FLEXCO_ATTN_ITEM_TILES / NW;      // of a wavefront
+constexpr int TILES = FLEXCO_ATTN_ITEM_TILES / CHUNK_NW;      // of a wavefront
 
 // pos: the columns' own positions (-1: no column), first: the item's first position, end: one past its last, all relative to the
 // block's key range
@@ -401,11 +401,14 @@ __device__ inline void chunk_step(const Args& a, const Tables& tab, const StepLd
   }
 }
 
-// MODE: 1 single tokens only, 2 chunks only, 3 both
-template <int MODE>
-__global__ __launch_bounds__(NT, 2) void kv8_attn_kernel(Args a) {
+// MODE: 1 single tokens only, 2 chunks only, 3 both.  NW: wavefronts of a block (chunks: two)
+template <int MODE, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
+  static_assert(MODE == 1 || NW == CHUNK_NW, "a chunk's four tiles are two wavefronts' work");
+  constexpr int NT = 64 * NW;
   __shared__ Tables tab;
   __shared__ __attribute__((aligned(1024))) StepLds ring0, ring1;
+  __shared__ float token_o[MODE == 1 ? NW * 16 * D : 4];
   __shared__ float token_m[NW][16], token_l[NW][16];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -451,9 +454,9 @@ __global__ __launch_bounds__(NT, 2) void kv8_attn_kernel(Args a) {
     __syncthreads();
   };
   if (MODE == 1 || (MODE == 3 && lone)) {
-    static_assert(sizeof(StepLds) >= NW * 16 * D * sizeof(float), "the sums of a single token fit a step's buffer");
-    const TokenLds token{reinterpret_cast<float*>(ring0.k), token_m, token_l};
-    token_block(a, tab, token, tile0, split, fold, kvh, npg, min(last_pos + 1 - pb * PS, npg * PS), keep_scales);
+    static_assert(MODE == 1 || sizeof(StepLds) >= NW * 16 * D * sizeof(float), "the sums of a single token fit a step's buffer");
+    const TokenLds token{MODE == 1 ? token_o : reinterpret_cast<float*>(ring0.k), token_m, token_l};
+    token_block<NW>(a, tab, token, tile0, split, fold, kvh, npg, min(last_pos + 1 - pb * PS, npg * PS), keep_scales);
     return;
   }
   if constexpr (MODE != 1) {
@@ -584,8 +587,9 @@ __global__ __launch_bounds__(32 * MG) void kv8_merge_long_kernel(Args a, const i
 
 int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
                                   float* part_ml, float* part_acc, void* out, size_t ldo, float* lse, hipStream_t s,
-                                  const AttnKeep* keep, int fold) {
-  const int group = c.n_q_heads / c.n_kv_heads;
+                                  const AttnKeep* keep) {
+  const Kv8Plan plan = plan_kv8_attention(m, c.n_kv_heads);
+  const int fold = plan.fold, group = c.n_q_heads / c.n_kv_heads;
   if (c.dtype != FLEXCO_BF16 || c.head_dim != D || c.page_size != PS || group > 16 || ldq % 8 != 0 ||
       m.kv_split_pages * fold > MAXSP || ldo % 4 != 0 || ((uintptr_t)out & 7))
     return FLEXCO_EUNSUPPORTED;
@@ -604,9 +608,14 @@ int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& 
   const dim3 grid((unsigned)turns_of(m.n_items, fold) * c.n_kv_heads);
   {
     KernelTimerScope ts(FLEXCO_K_ATTN_FWD, s);
-    if (m.n_single == m.n_items) hipLaunchKernelGGL(kv8_attn_kernel<1>, grid, dim3(NT), 0, s, a);
-    else if (m.n_single == 0) hipLaunchKernelGGL(kv8_attn_kernel<2>, grid, dim3(NT), 0, s, a);
-    else hipLaunchKernelGGL(kv8_attn_kernel<3>, grid, dim3(NT), 0, s, a);
+    if (m.n_single == m.n_items) {
+      if (plan.wavefronts == 4) hipLaunchKernelGGL((kv8_attn_kernel<1, 4>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((kv8_attn_kernel<1, 2>), grid, dim3(128), 0, s, a);
+    } else if (m.n_single == 0) {
+      hipLaunchKernelGGL((kv8_attn_kernel<2, CHUNK_NW>), grid, dim3(64 * CHUNK_NW), 0, s, a);
+    } else {
+      hipLaunchKernelGGL((kv8_attn_kernel<3, CHUNK_NW>), grid, dim3(64 * CHUNK_NW), 0, s, a);
+    }
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FLEXCO_EHIP, "launch of kv8_attn failed: %s", hipGetErrorString(e));

@@ -15,10 +15,9 @@ int32_t launch_kv8_attention_generic(const flexco_layer_cfg& c, const flexco_map
                                      const flexco_kv8_pool& pool, float* part_ml, float* part_acc, void* out, size_t ldo, float* lse,
                                      hipStream_t s, const AttnKeep* keep);
 
-// (with the joining of partial rows) bf16, head_dim 128, page_size 16, at most 16 query heads per kv head; otherwise FLEXCO_EUNSUPPORTED without launching.  fold: key
-// splits of a request of one token that one block takes as one (the others' partial rows stay unwritten)
+// (with the joining of partial rows) bf16, head_dim 128, page_size 16, at most 16 query heads per kv head; otherwise FLEXCO_EUNSUPPORTED without launching
 int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
                                   float* part_ml, float* part_acc, void* out, size_t ldo, float* lse, hipStream_t s,
-                                  const AttnKeep* keep, int fold);
+                                  const AttnKeep* keep);
 
 }  // namespace flexco

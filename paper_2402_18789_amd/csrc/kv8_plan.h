@@ -1,6 +1,5 @@
 #pragma once
-// How many neighbouring key splits of the work list a block of the 8-bit attention takes as one (requests of one token).  Host
-// arithmetic on the maps' sums alone.
+// How the 8-bit attention cuts a work list for its blocks.  Host arithmetic on the maps' sums alone.
 #include <algorithm>
 #include <cstdint>
 #include "flexco.h"
@@ -9,29 +8,34 @@ namespace flexco {
 
 constexpr int KV8_MAX_PAGES = 512;        // pages of a block's table
 
-// The work list is cut for one wavefront per item and head; a block here has two, and four of them fit a CU: 1024 on the chip.
-// Us of attention and joining, one fold / another:
-//   * contexts of up to 48 pages stay whole: 64 requests of 30 - 500 keys 18.5 / 14.0, 16 of 300 10.9 / 8.5, one of 700 11.2 / 9.9 (up to 62
-//     pages level, 125 in one 15 against 11);
-//   * pieces of 8 and 16 pages are taken together while there are more blocks than the chip holds, up to 64 pages: one context of 32000
-//     28 / 22.7, three of 9001 - 32765 38 / 33.7, 32 requests of 100 - 1000 18 / 16.5; with fewer blocks they stay as they are (4 of 4000
-//     15.1 / 16.0, 12 of 700 - 1500 14.6 / 16);
-//   * longer pieces stay (64 requests of 500 - 4096 in pieces of 64 pages 65 / 72) unless whole requests fill the chip: 96 of 4000
-//     164 / 145.
-inline int plan_kv8_fold(const flexco_maps& m, int nkv) {
+// fold: neighbouring key splits of a request of one token that its block takes as one.  wavefronts: of a block of a list of nothing but single
+// tokens (chunks, and what lies in a list with them: two).
+struct Kv8Plan { int fold, wavefronts; };
+
+// The work list is cut for one wavefront per item and head, finer than blocks of several need.  Us of attention and joining, measured with
+// 1 - 512 requests of 50 - 32000 keys over 1 and 8 kv heads, every fold and 2, 4 and 8 wavefronts (8 were never ahead):
+//   * contexts of up to 64 pages stay whole, there is nothing to join: 4 of 1000 keys in eights 9.2, whole 8.4; 32 of 100 - 1000 20 / 14.1;
+//     125 pages whole 12.0, in 16s 9.3;
+//   * else pieces of 8 pages are joined to 16 where there are few (one context of 2000 9.3, 32s 10.2), to 32 (64 of 500 - 4096 over
+//     one head 22 / 17.8, 64s 20.3) or 64 (one of 32000 33 / 19.2) as their number grows, longer ones to 64 (three of 9001 - 32765 44 / 34.6,
+//     8 of 8000 34.8 / 32.0; in 128s 38);
+//   * whole requests of up to 256 pages that fill the chip stay whole: 96 of 4000 in 128s 149, whole 140.
+// Two wavefronts where there are more short pieces than the chip holds blocks of four (256 of 10 - 600 keys 37.8 / 44.1, 512 of 16 - 400
+// 52.9 / 68.6), else four (one context of 700 keys 10.0 / 7.9, 128 of 100 - 4096 112 / 100, 256 of 512 - 4096 215 / 213).
+inline Kv8Plan plan_kv8_attention(const flexco_maps& m, int nkv) {
   const int sp = m.kv_split_pages;
-  if (m.n_single == 0 || m.n_parts == m.n_tiles || sp <= 0) return 1;
-  auto up_to = [&](int pages) {
-    int f = 1;
-    while (f * sp < pages && 2 * f * sp <= KV8_MAX_PAGES) f *= 2;
-    return f;
-  };
-  if (m.max_pages <= 48) return up_to(m.max_pages);
-  if (m.n_single == m.n_items && m.max_pages <= 256 && (int64_t)m.n_tiles * nkv >= 768) return up_to(m.max_pages);
-  int f = 1;
-  if (sp <= 16)
-    while ((int64_t)m.n_single * nkv > 1100 * f && 2 * f * sp <= 64) f *= 2;
-  return f;
+  const bool alone = m.n_single == m.n_items;
+  if (m.n_single == 0 || sp <= 0) return {1, 2};
+  const int64_t blocks = (int64_t)m.n_single * nkv;
+  int pages = m.max_pages;                // of a piece
+  if (m.n_parts > m.n_tiles && m.max_pages > 64 && !(alone && m.max_pages <= 256 && (int64_t)m.n_tiles * nkv >= 768))
+    pages = sp > 8 || blocks > 1500 ? 64 : blocks > 512 ? 32 : 16;
+  int fold = 1;
+  if (m.n_parts > m.n_tiles)
+    while (fold * sp < pages && 2 * fold * sp <= KV8_MAX_PAGES) fold *= 2;
+  const int64_t left = (blocks + fold - 1) / fold;
+  const bool few_pages = (int64_t)m.stream_pages * nkv < 24 * left;
+  return {fold, alone && !(few_pages && left > 1024) ? 4 : 2};
 }
 
 }  // namespace flexco
