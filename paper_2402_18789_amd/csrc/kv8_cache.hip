@@ -22,6 +22,25 @@ __device__ inline void load8(const bf16_t* p, float* v) { Vec<bf16_t>::load(p, v
 __device__ inline void store8(float* p, const float* v) { Vec<float>::store(p, v); Vec<float>::store(p + 4, v + 4); }
 __device__ inline void store8(bf16_t* p, const float* v) { Vec<bf16_t>::store(p, v); }
 
+// eight elements as they lie in memory
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16_t> {
+  bf16x8 v;
+  __device__ void load(const bf16_t* p) { v = *reinterpret_cast<const bf16x8*>(p); }
+  __device__ void get(float* x) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+  }
+};
+template <> struct Raw8<float> {
+  f32x4 v[2];
+  __device__ void load(const float* p) { v[0] = *reinterpret_cast<const f32x4*>(p); v[1] = *reinterpret_cast<const f32x4*>(p + 4); }
+  __device__ void get(float* x) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = v[e / 4][e % 4];
+  }
+};
+
 struct AppendArgs {
   const int32_t *runs, *tok_pos, *slot;
   uint8_t *k_codes, *v_codes;
@@ -33,38 +52,60 @@ struct AppendArgs {
   void* q_cache;
 };
 
-// Cosine and sine of pair i's angle at position pos: the turn's distance to the nearest quarter, at most an eighth, and the Taylor series of
-// both there (x <= pi / 4: what is left out is below 5e-14).
-__device__ inline void cos_sin_64(const RopeFreq& f, int i, int pos, double* c, double* s) {
-  const double r = (double)pos * f.rev[i], turn = r - floor(r), quarter = rint(4.0 * turn);
+// Cosine and sine of an angle of pos * rev turns: the turn's distance to the nearest quarter, at most an eighth, and the Taylor series of
+// both there (x <= pi / 4: what is left out is below 2e-9, and the fp32 value of a key is off by 6e-8 anyway).
+__device__ inline void cos_sin_64(double rev, int pos, double* c, double* s) {
+  const double r = (double)pos * rev, turn = r - floor(r), quarter = rint(4.0 * turn);
   const double x = (turn - 0.25 * quarter) * 6.283185307179586476925, y = x * x;
-  const double sn = x * (1.0 + y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880 + y * (-1.0 / 39916800 + y * (1.0 / 6227020800.0)))))));
-  const double cs = 1.0 + y * (-0.5 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 + y * (-1.0 / 3628800 + y * (1.0 / 479001600.0 + y * (-1.0 / 87178291200.0)))))));
+  const double sn = x * (1.0 + y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880)))));
+  const double cs = 1.0 + y * (-0.5 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 + y * (-1.0 / 3628800)))));
   const int k = (int)quarter & 3;
   const double a = k & 1 ? sn : cs, b = k & 1 ? cs : sn;
   *c = k == 1 || k == 2 ? -a : a;
   *s = k >= 2 ? -b : b;
 }
 
-// cs: d / 2 cosines, then sines, of a token.  Eight pairs from channel ch < d / 2 on: x, y -> x c - y s, y c + x s
+// Eight pairs x, y (channels ch .. + 7 and d / 2 + ch .. + 7 of a head) turned: x c - y s, y c + x s
 template <typename F>
-__device__ inline void rotate8(const double* cs, int half, int ch, const float* x, const float* y, F* lo, F* hi) {
+struct Angles8 {
+  F c[8], s[8];
+  template <typename A>
+  __device__ Angles8(const A* cs, int half, int ch) {          // cs: d / 2 cosines, then sines, of a token
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const F c = (F)cs[ch + e], s = (F)cs[half + ch + e];
-    lo[e] = (F)x[e] * c - (F)y[e] * s;
-    hi[e] = (F)y[e] * c + (F)x[e] * s;
+    for (int e = 0; e < 8; ++e) { c[e] = (F)cs[ch + e]; s[e] = (F)cs[half + ch + e]; }
   }
+  __device__ void turn(const float* x, const float* y, float* lo, float* hi) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const F l = (F)x[e] * c[e] - (F)y[e] * s[e], h = (F)y[e] * c[e] + (F)x[e] * s[e];
+      lo[e] = (float)l;
+      hi[e] = (float)h;
+    }
+  }
+};
+// Largest magnitude of sixteen elements, those that are no finite number left out; all: there was none of these.  (x 0 summed is NaN
+// where one is infinite or NaN: a multiply-add per element instead of two comparisons in the two places that ask.)
+__device__ inline float largest16(const float* v, bool* all) {
+  float odd = 0.f, m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) odd = __builtin_fmaf(v[e], 0.f, odd);
+  *all = odd == odd;
+  if (*all) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(v[e]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, kv8_finite(v[e]) ? fabsf(v[e]) : 0.f);
+  }
+  return m;
 }
-__device__ inline float finite_abs(float v) { return kv8_finite(v) ? fabsf(v) : 0.f; }
 
+// turned queries of token t, head h, channels ch .. + 7 and d / 2 + ch .. + 7
 template <typename T>
-__device__ inline void query8(const AppendArgs& a, const double* cs, const T* row, T* q_out, int t, int h, int ch) {
+__device__ inline void put_query(const AppendArgs& a, const Angles8<float>& an, const float* x, const float* y, T* q_out, int t, int h, int ch) {
   const int half = a.d >> 1;
-  float x[8], y[8], lo[8], hi[8];
-  load8(row + (size_t)h * a.d + ch, x);
-  load8(row + (size_t)h * a.d + ch + half, y);
-  rotate8<float>(cs, half, ch, x, y, lo, hi);
+  float lo[8], hi[8];
+  an.turn(x, y, lo, hi);
   T* o = q_out + (size_t)t * a.ld_q + (size_t)h * a.d + ch;
   store8(o, lo);
   store8(o + half, hi);
@@ -74,10 +115,21 @@ __device__ inline void query8(const AppendArgs& a, const double* cs, const T* ro
     store8(o2 + half, hi);
   }
 }
-__device__ inline u32x2 encode8(const float* v, float inv) {
+template <typename T>
+__device__ inline void query8(const AppendArgs& a, const double* cs, const T* row, T* q_out, int t, int h, int ch) {
+  const int half = a.d >> 1;
+  float x[8], y[8];
+  load8(row + (size_t)h * a.d + ch, x);
+  load8(row + (size_t)h * a.d + ch + half, y);
+  put_query(a, Angles8<float>(cs, half, ch), x, y, q_out, t, h, ch);
+}
+__device__ inline u32x2 encode8(const float* v, float inv, bool all) {
   float w[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = kv8_storable(v[e]) * inv;
+  for (int e = 0; e < 8; ++e) w[e] = v[e] * inv;
+  if (!all)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = kv8_storable(w[e]);
   return u32x2{kv8_encode4(w), kv8_encode4(w + 4)};
 }
 template <typename T>
@@ -85,12 +137,9 @@ __device__ inline void key8(const AppendArgs& a, const double* cs, const T* row,
   const int half = a.d >> 1;
   const T* kr = row + (size_t)(a.nq + kvh) * a.d;
   float x[8], y[8];
-  double l[8], h[8];
   load8(kr + ch, x);
   load8(kr + ch + half, y);
-  rotate8<double>(cs, half, ch, x, y, l, h);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) { lo[e] = (float)l[e]; hi[e] = (float)h[e]; }
+  Angles8<double>(cs, half, ch).turn(x, y, lo, hi);
 }
 
 // Sixteen bytes of a page's codes (unit u of d ps / 16) times `by`, but for those of positions [at, at + n)
@@ -114,135 +163,185 @@ __device__ inline void rescale_unit(uint8_t* codes, int u, int ps, int at, int n
   *p = now;
 }
 
-// The scales of a run's page and head: of K and of V.  amax: bits of the largest magnitudes (LDS, order of positive floats is that of
-// their bits).
-struct Scales { float old_k, old_v, k, v; };
-__device__ inline Scales page_scales(const AppendArgs& a, size_t ph, int at, uint32_t amax_k, uint32_t amax_v) {
-  Scales s;
-  s.old_k = at ? a.k_scale[ph] : 0.f;
-  s.old_v = at ? a.v_scale[ph] : 0.f;
-  s.k = fmaxf(s.old_k, kv8_scale_for(__builtin_bit_cast(float, amax_k)));
-  s.v = fmaxf(s.old_v, kv8_scale_for(__builtin_bit_cast(float, amax_v)));
-  return s;
-}
+// A page's scale for a run whose largest magnitude has the bits amax (LDS: the order of positive floats is that of their bits); old: the
+// page's own, 0 where the run begins it
+__device__ inline float new_scale(float old, uint32_t amax) { return fmaxf(old, kv8_scale_for(__builtin_bit_cast(float, amax))); }
 
-// A run of one token: one block for all heads (a block per head had an eighth of its threads at work).
-template <typename T>
+// A run of one token: one block for all heads (a block per head had an eighth of its threads at work).  Elements are asked for before
+// the angles are computed: a thread holds a piece of a key or value head and QP of query heads; what is beyond that is read later.
+template <typename T, int QP>
 __device__ inline void append_token(const AppendArgs& a, const RopeFreq& freq, const T* qkv, T* q_out, int t, int page, int at, double* cs,
                                     uint32_t* amax) {
-  const int tid = threadIdx.x, d = a.d, half = d >> 1, pc = d / 16;
-  const T* row = qkv + (size_t)t * (a.nq + 2 * a.nkv) * d;
-  for (int h = tid; h < 2 * a.nkv; h += THREADS) amax[h] = 0;
-  for (int i = tid; i < half; i += THREADS) cos_sin_64(freq, i, a.tok_pos[t], &cs[i], &cs[half + i]);
-  __syncthreads();
-  const T* vrow = row + (size_t)(a.nq + a.nkv) * d;
-  for (int u = tid; u < 2 * a.nkv * pc; u += THREADS) {
-    const int h = u / pc % a.nkv, ch = u % pc * 8;
-    float v[16], m = 0.f;
-    if (u < a.nkv * pc) {
-      key8(a, cs, row, h, ch, v, v + 8);
-    } else {
-      load8(vrow + (size_t)h * d + 2 * ch, v);
-      load8(vrow + (size_t)h * d + 2 * ch + 8, v + 8);
-    }
+  const int tid = threadIdx.x, d = a.d, half = d >> 1, pc = d / 16, nkv = a.nkv;
+  const T* row = qkv + (size_t)t * (a.nq + 2 * nkv) * d;
+  float* old = reinterpret_cast<float*>(amax + 2 * nkv);             // [2 nkv]
+  const int n_kv = 2 * nkv * pc, n_q = a.nq * pc;                    // pieces: keys, then values; queries
+  const size_t ph0 = (size_t)page * nkv;
+  // piece u: sixteen channels of a value head, or of a key head before it is turned (ch .. + 7, d / 2 + ch .. + 7)
+  auto load_kv = [&](int u, float* v) {
+    const T* p = row + (size_t)(a.nq + u / pc) * d;                  // (key heads, then value heads)
+    const int ch = u % pc * 8;
+    load8(p + (u < nkv * pc ? ch : 2 * ch), v);
+    load8(p + (u < nkv * pc ? ch + half : 2 * ch + 8), v + 8);
+  };
+  float kv[16];
+  Raw8<T> qx[QP ? QP : 1][2];
+  bool all = true;
+  if (tid < n_kv) load_kv(tid, kv);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) m = fmaxf(m, finite_abs(v[e]));
-    atomicMax(&amax[u < a.nkv * pc ? h : a.nkv + h], __builtin_bit_cast(uint32_t, m));
+  for (int i = 0; i < QP; ++i)
+    if (tid + i * THREADS < n_q) {
+      const T* p = row + (size_t)((tid + i * THREADS) / pc) * d + (tid + i * THREADS) % pc * 8;
+      qx[i][0].load(p);
+      qx[i][1].load(p + half);
+    }
+  for (int h = tid; h < 2 * nkv; h += THREADS) {
+    old[h] = !at ? 0.f : h < nkv ? a.k_scale[ph0 + h] : a.v_scale[ph0 + h - nkv];
+    amax[h] = 0;
   }
+  for (int i = tid; i < half; i += THREADS) cos_sin_64(freq.rev[i], a.tok_pos[t], &cs[i], &cs[half + i]);
   __syncthreads();
-  // (old scales are read here by every thread of a head and written behind the next barrier)
-  for (int u = tid; u < 2 * a.nkv * pc; u += THREADS) {
-    const int h = u / pc % a.nkv, ch = u % pc * 8;
-    const size_t ph = (size_t)page * a.nkv + h;
-    const Scales s = page_scales(a, ph, at, amax[h], amax[a.nkv + h]);
-    float v[16];
-    if (u < a.nkv * pc) {
-      key8(a, cs, row, h, ch, v, v + 8);
+  auto turned_kv = [&](int u, float* v) {                           // (a key piece in its place, the rest as it is)
+    if (u >= nkv * pc) return;
+    float lo[8], hi[8];
+    Angles8<double>(cs, half, u % pc * 8).turn(v, v + 8, lo, hi);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { v[e] = lo[e]; v[8 + e] = hi[e]; }
+  };
+  for (int u = tid; u < n_kv; u += THREADS) {
+    float v[16], m;
+    if (u == tid) {
+      turned_kv(u, kv);
+      m = largest16(kv, &all);
+    } else {
+      bool there;
+      load_kv(u, v);
+      turned_kv(u, v);
+      m = largest16(v, &there);
+    }
+    atomicMax(&amax[u / pc], __builtin_bit_cast(uint32_t, m));
+  }
+#pragma unroll
+  for (int i = 0; i < QP; ++i) {
+    const int u = tid + i * THREADS, ch = u % pc * 8;
+    if (u < n_q) {
+      float y[16];
+      qx[i][0].get(y);
+      qx[i][1].get(y + 8);
+      put_query(a, Angles8<float>(cs, half, ch), y, y + 8, q_out, t, u / pc, ch);
+    }
+  }
+  for (int u = tid + QP * THREADS; u < n_q; u += THREADS) query8(a, cs, row, q_out, t, u / pc, u % pc * 8);
+  __syncthreads();
+  auto put_kv = [&](int u, const float* p, bool finite) {
+    const int h = u / pc, ch = u % pc * 8;
+    const size_t ph = ph0 + h % nkv;
+    const float inv = 1.f / new_scale(old[h], amax[h]);
+    const u32x2 w[2] = {encode8(p, inv, finite), encode8(p + 8, inv, finite)};
+    if (h < nkv) {
       uint8_t* kc = a.k_codes + ph * a.ps * d;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int c = ch + x * half;
-        *reinterpret_cast<u32x2*>(kc + ((size_t)(c / 16) * a.ps + at) * 16 + c % 16) = encode8(v + 8 * x, 1.f / s.k);
+        *reinterpret_cast<u32x2*>(kc + ((size_t)(c / 16) * a.ps + at) * 16 + c % 16) = w[x];
       }
     } else {
-      load8(vrow + (size_t)h * d + 2 * ch, v);
-      load8(vrow + (size_t)h * d + 2 * ch + 8, v + 8);
       uint8_t* vc = a.v_codes + ph * a.ps * d + at;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const u32x2 w = encode8(v + 8 * x, 1.f / s.v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vc[(size_t)(2 * ch + 8 * x + e) * a.ps] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
-      }
+      for (int e = 0; e < 16; ++e) vc[(size_t)(2 * ch + e) * a.ps] = (uint8_t)(w[e / 8][e / 4 % 2] >> (8 * (e % 4)));
     }
+  };
+  if (tid < n_kv) put_kv(tid, kv, all);
+  for (int u = tid + THREADS; u < n_kv; u += THREADS) {
+    float v[16];
+    load_kv(u, v);
+    turned_kv(u, v);
+    put_kv(u, v, false);
   }
-  for (int u = tid; u < a.nq * pc; u += THREADS) query8(a, cs, row, q_out, t, u / pc, u % pc * 8);
-  __syncthreads();
-  if (at) {
-    const int units = d * a.ps / 16;
-    for (int i = tid; i < 2 * a.nkv * units; i += THREADS) {
-      const int h = i / units % a.nkv;
-      const bool keys = i < a.nkv * units;
-      const size_t ph = (size_t)page * a.nkv + h;
-      const Scales s = page_scales(a, ph, at, amax[h], amax[a.nkv + h]);
-      if (keys ? s.k > s.old_k : s.v > s.old_v)
-        rescale_unit((keys ? a.k_codes : a.v_codes) + ph * a.ps * d, i % units, a.ps, at, 1, keys ? s.old_k / s.k : s.old_v / s.v, keys);
-    }
-  }
-  __syncthreads();
-  for (int h = tid; h < a.nkv; h += THREADS) {
-    const size_t ph = (size_t)page * a.nkv + h;
-    const Scales s = page_scales(a, ph, at, amax[h], amax[a.nkv + h]);
-    a.k_scale[ph] = s.k;
-    a.v_scale[ph] = s.v;
+  for (int h = tid; h < 2 * nkv; h += THREADS) (h < nkv ? a.k_scale : a.v_scale)[ph0 + h % nkv] = new_scale(old[h], amax[h]);
+  if (!at) return;
+  __syncthreads();                       // (a unit of values holds the new position as well)
+  const int units = d * a.ps / 16;
+  for (int h = 0; h < 2 * nkv; ++h) {
+    const float s = new_scale(old[h], amax[h]);
+    if (!(s > old[h])) continue;                                     // (whole block)
+    for (int u = tid; u < units; u += THREADS)
+      rescale_unit((h < nkv ? a.k_codes : a.v_codes) + (ph0 + h % nkv) * a.ps * d, u, a.ps, at, 1, old[h] / s, h < nkv);
   }
 }
 
-// A run's page of sixteen positions, head_dim up to 128: half the block's threads hold the keys, half the values, sixteen elements
-// each, from their load to their codes, which go to memory through an image of the page in LDS: 16 bytes at a time.
-template <typename T>
+// A run's page of sixteen positions, head_dim 16 PC up to 128: half the block's threads hold the keys, half the values, sixteen elements
+// each, from their load to their codes, which go to memory through an image of the page in LDS: 16 bytes at a time.  A thread's queries
+// are those of its position and channels, so that it reads their angles once.
+template <typename T, int PC>
 __device__ inline void append_page16(const AppendArgs& a, const RopeFreq& freq, const T* qkv, T* q_out, int t0, int n, int kvh, int page,
-                                     int at, double* cs, uint32_t* amax) {
-  __shared__ __attribute__((aligned(16))) uint8_t image[2][16 * 128];
-  const int tid = threadIdx.x, d = a.d, half = d >> 1, pc = d / 16, group = a.nq / a.nkv;
+                                     int at, float* cs, uint32_t* amax) {
+  __shared__ __attribute__((aligned(16))) uint8_t image[2][16 * 16 * PC];
+  constexpr int d = 16 * PC, half = d / 2;
+  const int tid = threadIdx.x, group = a.nq / a.nkv;
   const size_t row_el = (size_t)(a.nq + 2 * a.nkv) * d, ph = (size_t)page * a.nkv + kvh;
-  const T* rows = qkv + (size_t)t0 * row_el;
   const bool keys = tid < THREADS / 2;
-  const int u = tid % (THREADS / 2), tl = u / pc, ch = u % pc * 8;
-  const bool mine = u < n * pc;
+  const int u = tid % (THREADS / 2), tl = u / PC, ch = u % PC * 8;
+  const bool mine = u < n * PC;
+  const T* row = qkv + (size_t)(t0 + (mine ? tl : 0)) * row_el;
   // (everything that needs nothing but the run is asked for before the angles)
   float x[16];
-  const T* src = rows + (size_t)tl * row_el + (size_t)(keys ? a.nq + kvh : a.nq + a.nkv + kvh) * d;
-  if (mine) {
-    load8(src + (keys ? ch : 2 * ch), x);
-    load8(src + (keys ? ch + half : 2 * ch + 8), x + 8);
+  Raw8<T> q0, q1;
+  const T* src = row + (size_t)(keys ? a.nq + kvh : a.nq + a.nkv + kvh) * d;
+  load8(src + (keys ? ch : 2 * ch), x);
+  load8(src + (keys ? ch + half : 2 * ch + 8), x + 8);
+  const T* qrow = row + (size_t)(kvh * group) * d + ch;
+  const int h0 = keys ? 1 : 0;                 // every other query head, the value half's share the larger
+  if (h0 < group) {
+    q0.load(qrow + h0 * d);
+    q1.load(qrow + h0 * d + half);
   }
   const float old_k = at ? a.k_scale[ph] : 0.f, old_v = at ? a.v_scale[ph] : 0.f;
   if (tid < 2) amax[tid] = 0;
-  for (int i = tid; i < n * half; i += THREADS) cos_sin_64(freq, i % half, a.tok_pos[t0 + i / half], &cs[i / half * d + i % half], &cs[i / half * d + half + i % half]);
-  __syncthreads();
+  // a key's thread computes the angles of its position and channels, in double precision for the key, and leaves them for the queries
   float m = 0.f;
+  bool all = true;
   if (mine) {
     if (keys) {
-      double l[8], h[8];
-      rotate8<double>(cs + tl * d, half, ch, x, x + 8, l, h);
+      const int pos = a.tok_pos[t0] + tl;                            // (a run's positions follow one another)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { x[e] = (float)l[e]; x[8 + e] = (float)h[e]; }
+      for (int e = 0; e < 8; ++e) {
+        double c, sn;
+        cos_sin_64(freq.rev[ch + e], pos, &c, &sn);
+        const double lo = x[e] * c - x[8 + e] * sn, hi = x[8 + e] * c + x[e] * sn;
+        x[e] = (float)lo;
+        x[8 + e] = (float)hi;
+        cs[tl * d + ch + e] = (float)c;
+        cs[tl * d + half + ch + e] = (float)sn;
+      }
     }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) m = fmaxf(m, finite_abs(x[e]));
+    m = largest16(x, &all);
   }
+  __syncthreads();
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
   if ((tid & 63) == 0) atomicMax(&amax[keys ? 0 : 1], __builtin_bit_cast(uint32_t, m));
+  if (mine) {
+    const Angles8<float> an(cs + tl * d, half, ch);
+    for (int h = h0; h < group; h += 2) {
+      float y[16];
+      q0.get(y);
+      q1.get(y + 8);
+      if (h + 2 < group) {
+        q0.load(qrow + (h + 2) * d);
+        q1.load(qrow + (h + 2) * d + half);
+      }
+      put_query(a, an, y, y + 8, q_out, t0 + tl, kvh * group + h, ch);
+    }
+  }
   __syncthreads();
-  const float s_k = fmaxf(old_k, kv8_scale_for(__builtin_bit_cast(float, amax[0]))), s_v = fmaxf(old_v, kv8_scale_for(__builtin_bit_cast(float, amax[1])));
+  const float s_k = new_scale(old_k, amax[0]), s_v = new_scale(old_v, amax[1]);
   if (tid == 0) { a.k_scale[ph] = s_k; a.v_scale[ph] = s_v; }
   if (mine) {
     const float inv = 1.f / (keys ? s_k : s_v);
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const u32x2 w = encode8(x + 8 * y, inv);
+      const u32x2 w = encode8(x + 8 * y, inv, all);
       if (keys) {
         const int c = ch + y * half;
         *reinterpret_cast<u32x2*>(&image[0][(c / 16 * 16 + at + tl) * 16 + c % 16]) = w;
@@ -252,13 +351,9 @@ __device__ inline void append_page16(const AppendArgs& a, const RopeFreq& freq, 
       }
     }
   }
-  for (int i = tid; i < n * group * pc; i += THREADS) {
-    const int qt = i / (group * pc), h = kvh * group + i / pc % group;
-    query8(a, cs + qt * d, rows + (size_t)qt * row_el, q_out, t0 + qt, h, i % pc * 8);
-  }
   __syncthreads();
   // a unit: sixteen channels of a position (keys), sixteen positions of a channel (values)
-  if (u >= pc * 16) return;
+  if (u >= PC * 16) return;
   uint8_t* to = (keys ? a.k_codes : a.v_codes) + ph * 16 * d + (size_t)u * 16;
   u32x4 w = *reinterpret_cast<const u32x4*>(&image[keys ? 0 : 1][u * 16]);
   const bool grew = at && (keys ? s_k > old_k : s_v > old_v);
@@ -301,7 +396,7 @@ __device__ inline void append_any(const AppendArgs& a, const RopeFreq& freq, con
   auto angles = [&](int g0, int gn) {
     __syncthreads();
     for (int i = tid; i < gn * half; i += THREADS)
-      cos_sin_64(freq, i % half, a.tok_pos[t0 + g0 + i / half], &cs[i / half * d + i % half], &cs[i / half * d + half + i % half]);
+      cos_sin_64(freq.rev[i % half], a.tok_pos[t0 + g0 + i / half], &cs[i / half * d + i % half], &cs[i / half * d + half + i % half]);
     __syncthreads();
   };
   for (int g0 = 0; g0 < n; g0 += GROUP) {
@@ -315,27 +410,27 @@ __device__ inline void append_any(const AppendArgs& a, const RopeFreq& freq, con
       const int tl = u / pc, ch = u % pc * 8;
       const T* row = rows + (size_t)(g0 + tl) * row_el;
       float v[16];
+      bool all;
       key8(a, cs + tl * d, row, kvh, ch, v, v + 8);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mk = fmaxf(mk, finite_abs(v[e]));
+      mk = fmaxf(mk, largest16(v, &all));
       load8(row + v_col + 2 * ch, v);
       load8(row + v_col + 2 * ch + 8, v + 8);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mv = fmaxf(mv, finite_abs(v[e]));
+      mv = fmaxf(mv, largest16(v, &all));
     }
   }
   atomicMax(&amax[0], __builtin_bit_cast(uint32_t, mk));
   atomicMax(&amax[1], __builtin_bit_cast(uint32_t, mv));
   __syncthreads();
-  const Scales s = page_scales(a, ph, at, amax[0], amax[1]);
+  const float old_k = at ? a.k_scale[ph] : 0.f, old_v = at ? a.v_scale[ph] : 0.f;
+  const float s_k = new_scale(old_k, amax[0]), s_v = new_scale(old_v, amax[1]);
   __syncthreads();                       // (every thread has read the old scales)
-  if (tid == 0) { a.k_scale[ph] = s.k; a.v_scale[ph] = s.v; }
+  if (tid == 0) { a.k_scale[ph] = s_k; a.v_scale[ph] = s_v; }
   uint8_t* kc = a.k_codes + ph * ps * d;
   uint8_t* vc = a.v_codes + ph * ps * d;
   if (at)
     for (int u = tid; u < d * ps / 16; u += THREADS) {
-      if (s.k > s.old_k) rescale_unit(kc, u, ps, at, n, s.old_k / s.k, true);
-      if (s.v > s.old_v) rescale_unit(vc, u, ps, at, n, s.old_v / s.v, false);
+      if (s_k > old_k) rescale_unit(kc, u, ps, at, n, old_k / s_k, true);
+      if (s_v > old_v) rescale_unit(vc, u, ps, at, n, old_v / s_v, false);
     }
   __syncthreads();                       // (a unit of values may hold new positions as well)
   for (int g0 = 0; g0 < n; g0 += GROUP) {
@@ -348,33 +443,33 @@ __device__ inline void append_any(const AppendArgs& a, const RopeFreq& freq, con
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int c = ch + x * half;
-        *reinterpret_cast<u32x2*>(kc + ((size_t)(c / 16) * ps + at + g0 + tl) * 16 + c % 16) = encode8(v + 8 * x, 1.f / s.k);
+        *reinterpret_cast<u32x2*>(kc + ((size_t)(c / 16) * ps + at + g0 + tl) * 16 + c % 16) = encode8(v + 8 * x, 1.f / s_k, false);
       }
     }
     for (int u = tid; u < gn * d; u += THREADS) {
       const int tl = u / d, ch = u % d;
-      const float v[4] = {kv8_storable(ld(rows + (size_t)(g0 + tl) * row_el + v_col + ch)) * (1.f / s.v), 0.f, 0.f, 0.f};
+      const float v[4] = {kv8_storable(ld(rows + (size_t)(g0 + tl) * row_el + v_col + ch)) * (1.f / s_v), 0.f, 0.f, 0.f};
       vc[(size_t)ch * ps + at + g0 + tl] = (uint8_t)kv8_encode4(v);
     }
   }
 }
 
-// FORM 0: every run is one token, a block each.  1: pages of sixteen, head_dim up to 128; 2: any; a block per (run, kv head), runs of one
-// token to the first head's.
+// FORM 0: every run is one token, a block each.  Else a block per (run, kv head), runs of one token to the first head's; FORM 4, 8: pages of
+// sixteen, head_dim 16 FORM; 1: any.
 template <typename T, int FORM>
 __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeFreq freq, const T* qkv, T* q_out) {
-  extern __shared__ double cs[];              // [tokens][d] angles, then 2 nkv largest magnitudes
+  extern __shared__ double cs[];              // [tokens][d] angles (pages of sixteen: fp32); then 2 nkv largest magnitudes, as many old scales
   const int run = FORM == 0 ? blockIdx.x : blockIdx.x / a.nkv, kvh = FORM == 0 ? 0 : blockIdx.x % a.nkv;
   const int t0 = a.runs[2 * run], n = a.runs[2 * run + 1];
   if (t0 < 0 || n < 1 || n > a.ps || t0 > a.T - n) return;              // (whole block, as below)
   const int sl = a.slot[t0], page = sl / a.ps, at = sl % a.ps;
   if (sl < 0 || page >= a.num_pages || at + n > a.ps) return;
-  uint32_t* amax = reinterpret_cast<uint32_t*>(cs + (FORM == 0 ? 1 : GROUP) * a.d);
+  uint32_t* amax = reinterpret_cast<uint32_t*>(cs + (FORM == 0 ? 1 : FORM == 1 ? GROUP : GROUP / 2) * a.d);
   if (n == 1) {
-    if (kvh == 0) append_token(a, freq, qkv, q_out, t0, page, at, cs, amax);
+    if (kvh == 0) append_token<T, FORM == 0 ? 2 : 0>(a, freq, qkv, q_out, t0, page, at, cs, amax);
+  } else if constexpr (FORM >= 4) {
+    append_page16<T, FORM>(a, freq, qkv, q_out, t0, n, kvh, page, at, reinterpret_cast<float*>(cs), amax);
   } else if constexpr (FORM == 1) {
-    append_page16(a, freq, qkv, q_out, t0, n, kvh, page, at, cs, amax);
-  } else if constexpr (FORM == 2) {
     append_any(a, freq, qkv, q_out, t0, n, kvh, page, at, cs, amax);
   }
 }
@@ -432,17 +527,19 @@ int32_t launch_kv8_append(const flexco_layer_cfg& c, const flexco_maps& m, const
   FLEXCO_TRY(rope_freq(c, &freq));
   const AppendArgs a{runs, m.tok_pos, m.slot, pool.k_codes, pool.v_codes, pool.k_scale, pool.v_scale, n_runs, m.T, pool.num_pages,
                      pool.page_size, c.n_q_heads, c.n_kv_heads, c.head_dim, ld_q, m.ft_tok0, q_cache ? m.n_ft : 0, q_cache};
-  const int form = n_runs == m.T ? 0 : c.page_size == 16 && c.head_dim <= 128 ? 1 : 2;
+  const int form = n_runs == m.T ? 0 : c.page_size == 16 && c.head_dim == 128 ? 8 : c.page_size == 16 && c.head_dim == 64 ? 4 : 1;
   const dim3 grid(form == 0 ? (unsigned)n_runs : (unsigned)n_runs * c.n_kv_heads);
-  const size_t shm = sizeof(double) * (form == 0 ? 1 : GROUP) * c.head_dim + sizeof(uint32_t) * 2 * c.n_kv_heads;
+  const size_t shm = sizeof(double) * (form == 0 ? 1 : form == 1 ? GROUP : GROUP / 2) * c.head_dim + 4 * sizeof(uint32_t) * c.n_kv_heads;
   if (shm > 48 * 1024) return fail(FLEXCO_EUNSUPPORTED, "8-bit append: %d kv heads of %d are too many", c.n_kv_heads, c.head_dim);
 #define FLEXCO_KV8_APPEND(T_, FORM_) \
   hipLaunchKernelGGL((kv8_append_kernel<T_, FORM_>), grid, dim3(THREADS), shm, s, a, freq, (const T_*)qkv, (T_*)q_out)
-  if (c.dtype == FLEXCO_BF16) {
-    if (form == 0) FLEXCO_KV8_APPEND(bf16_t, 0); else if (form == 1) FLEXCO_KV8_APPEND(bf16_t, 1); else FLEXCO_KV8_APPEND(bf16_t, 2);
-  } else {
-    if (form == 0) FLEXCO_KV8_APPEND(float, 0); else if (form == 1) FLEXCO_KV8_APPEND(float, 1); else FLEXCO_KV8_APPEND(float, 2);
-  }
+#define FLEXCO_KV8_APPEND_FORMS(T_)                  \
+  if (form == 0) FLEXCO_KV8_APPEND(T_, 0);           \
+  else if (form == 8) FLEXCO_KV8_APPEND(T_, 8);      \
+  else if (form == 4) FLEXCO_KV8_APPEND(T_, 4);      \
+  else FLEXCO_KV8_APPEND(T_, 1);
+  if (c.dtype == FLEXCO_BF16) { FLEXCO_KV8_APPEND_FORMS(bf16_t) } else { FLEXCO_KV8_APPEND_FORMS(float) }
+#undef FLEXCO_KV8_APPEND_FORMS
 #undef FLEXCO_KV8_APPEND
   return post("kv8_append");
 }
