@@ -102,37 +102,40 @@ struct Column {
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i], q[i], acc, 0, 0, 0);
     return acc;
   }
-  // Softmax of the raw scores of a step's four pages; leaves the probabilities as the second product takes them.  Any reference point gives
-  // the same row in the end: it follows the maximum only when that has moved by more than LAG, in one branch for the wavefront.
-  __device__ void softmax(const f32x4 (&acc)[SP], float scale_log2, bf16x8& p0, bf16x8& p1) {
+  // Softmax of the raw scores of a step's four pages, in two halves: the largest score (log2), and the probabilities as the second
+  // product takes them.  Any reference point gives the same row in the end: it follows the maximum only when that has moved by more than
+  // LAG (between the halves, in one branch for the wavefront).
+  __device__ static float largest(const f32x4 (&acc)[SP], float scale_log2) {
     float mx = acc[0][0];
 #pragma unroll
     for (int n = 0; n < SP; ++n)
 #pragma unroll
       for (int j = 0; j < 4; ++j) mx = fmaxf(mx, acc[n][j]);
-    mx = max_xor32(max_xor16(mx)) * scale_log2;
-    if (__builtin_amdgcn_ballot_w64(mx > m + LAG) != 0) {
-      const float m_new = mx > m + LAG ? mx : m, alpha = __builtin_amdgcn_exp2f(m - m_new);
-      m = m_new;
-      l *= alpha;
+    return max_xor32(max_xor16(mx)) * scale_log2;
+  }
+  __device__ void follow(float mx) {
+    const float m_new = mx > m + LAG ? mx : m, alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= alpha;
 #pragma unroll
-      for (int mt = 0; mt < 8; ++mt)
+    for (int mt = 0; mt < 8; ++mt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[mt][j] *= alpha;
-    }
+      for (int j = 0; j < 4; ++j) o[mt][j] *= alpha;
+  }
+  __device__ void probabilities(const f32x4 (&acc)[SP], float scale_log2, bf16x8& p0, bf16x8& p1) {
     uint32_t w0[SP], w1[SP];
+    float sum[SP];
 #pragma unroll
     for (int n = 0; n < SP; ++n) {
       float p[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[n][j], scale_log2, -m));
-        l += p[j];
-      }
+      for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[n][j], scale_log2, -m));
+      sum[n] = (p[0] + p[1]) + (p[2] + p[3]);
       const bf16x2 a = {(bf16_t)p[0], (bf16_t)p[1]}, b = {(bf16_t)p[2], (bf16_t)p[3]};
       w0[n] = __builtin_bit_cast(uint32_t, a);
       w1[n] = __builtin_bit_cast(uint32_t, b);
     }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     turn_words(w0);                          // word j: keys 4 j, 4 j + 1 of the lane's page ...
     turn_words(w1);                          // ... and 4 j + 2, 4 j + 3
     p0 = __builtin_bit_cast(bf16x8, u32x4{w0[0], w1[0], w0[1], w1[1]});
@@ -245,7 +248,9 @@ __device__ inline void token_block(const Args& a, const Tables& tab, const Token
         for (int i = 0; i < 4; ++i) v[mt][i] &= first_bytes(left - 4 * i);
     }
     bf16x8 p0, p1;
-    col.softmax(acc, a.scale_log2, p0, p1);
+    const float mx = Column::largest(acc, a.scale_log2);
+    if (__builtin_amdgcn_ballot_w64(mx > col.m + LAG) != 0) col.follow(mx);
+    col.probabilities(acc, a.scale_log2, p0, p1);
     const float vs = tab.vs[min(SP * st + g, npg - 1)];
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) {
@@ -318,15 +323,16 @@ __device__ inline void load_step(const Args& a, const Tables& tab, StepLds& to, 
 
 constexpr int TILES = FLEXCO_ATTN_ITEM_TILES / CHUNK_NW;      // of a wavefront
 
-// pos: the columns' own positions (-1: no column), first: the item's first position, end: one past its last, all relative to the
-// block's key range
-__device__ inline void chunk_step(const Args& a, const Tables& tab, const StepLds& in, Column (&col)[TILES], int tiles, int st, int npg,
-                                  const int (&pos)[TILES], int first, int end, int lane) {
+// EDGE: a key of the step may lie behind some column's position or the block's range (else no mask, no clearing).  pos: the columns' own
+// positions (-1: no column), end: one past the item's last, both relative to the block's key range
+template <bool EDGE>
+__device__ inline void chunk_step(float scale_log2, const Tables& tab, const StepLds& in, Column (&col)[TILES], int st, int npg,
+                                  const int (&pos)[TILES], int end, int lane) {
   const int c = lane & 15, g = lane >> 4;
   f32x4 acc[TILES][SP];
 #pragma unroll
   for (int n = 0; n < SP; ++n) {
-    const float ks = tab.ks[min(SP * st + n, npg - 1)];
+    const float ks = tab.ks[EDGE ? min(SP * st + n, npg - 1) : SP * st + n];
     bf16x8 kf[4];
     widen(*reinterpret_cast<const u32x4*>(in.k + n * PAGE + lane * 16), ks, kf[0], kf[1]);
     widen(*reinterpret_cast<const u32x4*>(in.k + n * PAGE + 1024 + lane * 16), ks, kf[2], kf[3]);
@@ -334,8 +340,7 @@ __device__ inline void chunk_step(const Args& a, const Tables& tab, const StepLd
     for (int x = 0; x < TILES; ++x) acc[x][n] = col[x].scores(kf);
   }
   const int k0 = SP * st * PS;
-  const bool edge = k0 + SP * PS > min(first + 1, npg * PS);        // a key here lies behind some column's position, or the range
-  if (edge) {
+  if constexpr (EDGE) {
 #pragma unroll
     for (int x = 0; x < TILES; ++x)
 #pragma unroll
@@ -347,11 +352,22 @@ __device__ inline void chunk_step(const Args& a, const Tables& tab, const StepLd
         }
   }
   bf16x8 p0[TILES], p1[TILES];
+  // (one branch for all tiles: what follows it is one block, in which a tile's exponentials run beside another's products)
+  float mx[TILES];
+  bool moved = false;
 #pragma unroll
-  for (int x = 0; x < TILES; ++x) col[x].softmax(acc[x], a.scale_log2, p0[x], p1[x]);
-  const float vs = tab.vs[min(SP * st + g, npg - 1)];
+  for (int x = 0; x < TILES; ++x) {
+    mx[x] = Column::largest(acc[x], scale_log2);
+    moved |= mx[x] > col[x].m + LAG;
+  }
+  if (__builtin_amdgcn_ballot_w64(moved) != 0)
+#pragma unroll
+    for (int x = 0; x < TILES; ++x) col[x].follow(mx[x]);
+#pragma unroll
+  for (int x = 0; x < TILES; ++x) col[x].probabilities(acc[x], scale_log2, p0[x], p1[x]);
+  const float vs = tab.vs[EDGE ? min(SP * st + g, npg - 1) : SP * st + g];
   const uint8_t* vrow = in.v + g * PAGE + c * 16;
-  if (!edge) {
+  if constexpr (!EDGE) {
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) {
       bf16x8 v0, v1;
@@ -364,39 +380,44 @@ __device__ inline void chunk_step(const Args& a, const Tables& tab, const StepLd
   // slots behind the item's last position are cleared; NaN codes before it are taken out, and a product of their places with the
   // places that a column sees says whose rows they belong in
   const int left = min(end, npg * PS) - (k0 + g * PS);
+  uint32_t odd = 0;
 #pragma unroll
   for (int mt = 0; mt < 8; ++mt) {
-    u32x4 w = *reinterpret_cast<const u32x4*>(vrow + mt * 256), bad;
-    uint32_t here = 0;
+    u32x4 w = *reinterpret_cast<const u32x4*>(vrow + mt * 256);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       w[i] &= first_bytes(left - 4 * i);
       const uint32_t n = has_nan(w[i]);
-      here |= n;
-      bad[i] = bytes_of(n, 0x38u);                              // 1.0 where the code is NaN
+      odd |= n;
       w[i] &= ~bytes_of(n, 0xffu);
     }
     bf16x8 v0, v1;
     widen(w, vs, v0, v1);
 #pragma unroll
     for (int x = 0; x < TILES; ++x) col[x].add(mt, v0, v1, p0[x], p1[x]);
-    if (__builtin_amdgcn_ballot_w64(here != 0) != 0) {
-      widen(bad, 1.f, v0, v1);
+  }
+  if (__builtin_amdgcn_ballot_w64(odd != 0) == 0) return;
 #pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        bf16x8 s0, s1;
+  for (int x = 0; x < TILES; ++x) {
+    bf16x8 s0, s1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s0[i] = (bf16_t)(k0 + g * PS + i <= pos[x] ? 1.f : 0.f);
-          s1[i] = (bf16_t)(k0 + g * PS + 8 + i <= pos[x] ? 1.f : 0.f);
-        }
-        f32x4 n = {0.f, 0.f, 0.f, 0.f};
-        n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, s0, n, 0, 0, 0);
-        n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, s1, n, 0, 0, 0);
+    for (int i = 0; i < 8; ++i) {
+      s0[i] = (bf16_t)(k0 + g * PS + i <= pos[x] ? 1.f : 0.f);
+      s1[i] = (bf16_t)(k0 + g * PS + 8 + i <= pos[x] ? 1.f : 0.f);
+    }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (n[j] > 0.f) col[x].o[mt][j] = __builtin_nanf("");
-      }
+    for (int mt = 0; mt < 8; ++mt) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(vrow + mt * 256);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = bytes_of(has_nan(w[i] & first_bytes(left - 4 * i)), 0x38u);      // 1.0 where the code is NaN
+      bf16x8 v0, v1;
+      widen(w, 1.f, v0, v1);
+      f32x4 n = {0.f, 0.f, 0.f, 0.f};
+      n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, s0, n, 0, 0, 0);
+      n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, s1, n, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n[j] > 0.f) col[x].o[mt][j] = __builtin_nanf("");
     }
   }
 }
@@ -485,14 +506,26 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
     __builtin_amdgcn_s_barrier();             \
     asm volatile("" ::: "memory");            \
   }
-    for (int st = 0; st < n_st; st += 2) {
+    const float scale_log2 = a.scale_log2;
+    const bool work = tiles > 0;
+    // first the steps that lie wholly before every column's own position, in pairs, then the rest
+    int st = 0;
+    for (const int n_free = (min(first + 1, npg * PS) / (SP * PS)) & ~1; st < n_free; st += 2) {
+      FLEXCO_KV8_HAND_OVER()
+      load_step(a, tab, ring1, st + 1, kvh, npg, wave, lane);
+      if (work) chunk_step<false>(scale_log2, tab, ring0, col, st, npg, pos, end, lane);
+      FLEXCO_KV8_HAND_OVER()
+      if (st + 2 < n_st) load_step(a, tab, ring0, st + 2, kvh, npg, wave, lane);
+      if (work) chunk_step<false>(scale_log2, tab, ring1, col, st + 1, npg, pos, end, lane);
+    }
+    for (; st < n_st; st += 2) {
       FLEXCO_KV8_HAND_OVER()
       if (st + 1 < n_st) load_step(a, tab, ring1, st + 1, kvh, npg, wave, lane);
-      if (tiles > 0) chunk_step(a, tab, ring0, col, tiles, st, npg, pos, first, end, lane);
+      if (work) chunk_step<true>(scale_log2, tab, ring0, col, st, npg, pos, end, lane);
       if (st + 1 >= n_st) break;
       FLEXCO_KV8_HAND_OVER()
       if (st + 2 < n_st) load_step(a, tab, ring0, st + 2, kvh, npg, wave, lane);
-      if (tiles > 0) chunk_step(a, tab, ring1, col, tiles, st + 1, npg, pos, first, end, lane);
+      if (work) chunk_step<true>(scale_log2, tab, ring1, col, st + 1, npg, pos, end, lane);
     }
 #undef FLEXCO_KV8_HAND_OVER
 #pragma unroll
