@@ -32,7 +32,7 @@ constexpr int MAXSP = KV8_MAX_PAGES;     // pages of a block's key range at most
 constexpr int SP = 4;                    // pages of a step
 constexpr int CHUNK_NW = 2;              // wavefronts of a chunk's block
 constexpr float NO_KEY = -3.402823466e38f;   // the maximum of no key yet: finite, so that a masked score less this is still -inf
-constexpr float LAG = 8.f;               // how far (log2) a column's maximum may run ahead of its reference point
+constexpr float MOST = 256.f;            // the most that a lane's exponentials of a step may come to before the reference point follows the maximum
 #define FLEXCO_GP(p) ((const __attribute__((address_space(1))) void*)(p))
 #define FLEXCO_LP(p) ((__attribute__((address_space(3))) void*)(p))
 
@@ -102,19 +102,25 @@ struct Column {
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i], q[i], acc, 0, 0, 0);
     return acc;
   }
-  // Softmax of the raw scores of a step's four pages, in two halves: the largest score (log2), and the probabilities as the second
-  // product takes them.  Any reference point gives the same row in the end: it follows the maximum only when that has moved by more than
-  // LAG (between the halves, in one branch for the wavefront).
-  __device__ static float largest(const f32x4 (&acc)[SP], float scale_log2) {
+  // Softmax of the raw scores of a step's four pages in three parts.  Any reference point gives the same row in the end: it stays where it
+  // is unless a lane's sixteen exponentials come to more than MOST (or NaN), and the largest score is looked for only then.
+  __device__ float exponentials(const f32x4 (&acc)[SP], float scale_log2, f32x4 (&p)[SP]) const {
+    float sum[SP];
+#pragma unroll
+    for (int n = 0; n < SP; ++n) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[n][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[n][j], scale_log2, -m));
+      sum[n] = (p[n][0] + p[n][1]) + (p[n][2] + p[n][3]);
+    }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+  __device__ void follow(const f32x4 (&acc)[SP], float scale_log2) {
     float mx = acc[0][0];
 #pragma unroll
     for (int n = 0; n < SP; ++n)
 #pragma unroll
       for (int j = 0; j < 4; ++j) mx = fmaxf(mx, acc[n][j]);
-    return max_xor32(max_xor16(mx)) * scale_log2;
-  }
-  __device__ void follow(float mx) {
-    const float m_new = mx > m + LAG ? mx : m, alpha = __builtin_amdgcn_exp2f(m - m_new);
+    const float m_new = fmaxf(m, max_xor32(max_xor16(mx)) * scale_log2), alpha = __builtin_amdgcn_exp2f(m - m_new);
     m = m_new;
     l *= alpha;
 #pragma unroll
@@ -122,20 +128,15 @@ struct Column {
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[mt][j] *= alpha;
   }
-  __device__ void probabilities(const f32x4 (&acc)[SP], float scale_log2, bf16x8& p0, bf16x8& p1) {
+  // the probabilities as the second product takes them
+  __device__ static void turn(const f32x4 (&p)[SP], bf16x8& p0, bf16x8& p1) {
     uint32_t w0[SP], w1[SP];
-    float sum[SP];
 #pragma unroll
     for (int n = 0; n < SP; ++n) {
-      float p[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[n][j], scale_log2, -m));
-      sum[n] = (p[0] + p[1]) + (p[2] + p[3]);
-      const bf16x2 a = {(bf16_t)p[0], (bf16_t)p[1]}, b = {(bf16_t)p[2], (bf16_t)p[3]};
+      const bf16x2 a = {(bf16_t)p[n][0], (bf16_t)p[n][1]}, b = {(bf16_t)p[n][2], (bf16_t)p[n][3]};
       w0[n] = __builtin_bit_cast(uint32_t, a);
       w1[n] = __builtin_bit_cast(uint32_t, b);
     }
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     turn_words(w0);                          // word j: keys 4 j, 4 j + 1 of the lane's page ...
     turn_words(w1);                          // ... and 4 j + 2, 4 j + 3
     p0 = __builtin_bit_cast(bf16x8, u32x4{w0[0], w1[0], w0[1], w1[1]});
@@ -248,9 +249,14 @@ __device__ inline void token_block(const Args& a, const Tables& tab, const Token
         for (int i = 0; i < 4; ++i) v[mt][i] &= first_bytes(left - 4 * i);
     }
     bf16x8 p0, p1;
-    const float mx = Column::largest(acc, a.scale_log2);
-    if (__builtin_amdgcn_ballot_w64(mx > col.m + LAG) != 0) col.follow(mx);
-    col.probabilities(acc, a.scale_log2, p0, p1);
+    f32x4 p[SP];
+    float sum = col.exponentials(acc, a.scale_log2, p);
+    if (__builtin_amdgcn_ballot_w64(!(sum <= MOST)) != 0) {
+      col.follow(acc, a.scale_log2);
+      sum = col.exponentials(acc, a.scale_log2, p);
+    }
+    col.l += sum;
+    Column::turn(p, p0, p1);
     const float vs = tab.vs[min(SP * st + g, npg - 1)];
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) {
@@ -352,19 +358,25 @@ __device__ inline void chunk_step(float scale_log2, const Tables& tab, const Ste
         }
   }
   bf16x8 p0[TILES], p1[TILES];
-  // (one branch for all tiles: what follows it is one block, in which a tile's exponentials run beside another's products)
-  float mx[TILES];
-  bool moved = false;
+  f32x4 p[TILES][SP];
+  float sum[TILES];
+  bool more = false;
 #pragma unroll
   for (int x = 0; x < TILES; ++x) {
-    mx[x] = Column::largest(acc[x], scale_log2);
-    moved |= mx[x] > col[x].m + LAG;
+    sum[x] = col[x].exponentials(acc[x], scale_log2, p[x]);
+    more |= !(sum[x] <= MOST);
   }
-  if (__builtin_amdgcn_ballot_w64(moved) != 0)
+  if (__builtin_amdgcn_ballot_w64(more) != 0)      // (one branch for all tiles)
 #pragma unroll
-    for (int x = 0; x < TILES; ++x) col[x].follow(mx[x]);
+    for (int x = 0; x < TILES; ++x) {
+      col[x].follow(acc[x], scale_log2);
+      sum[x] = col[x].exponentials(acc[x], scale_log2, p[x]);
+    }
 #pragma unroll
-  for (int x = 0; x < TILES; ++x) col[x].probabilities(acc[x], scale_log2, p0[x], p1[x]);
+  for (int x = 0; x < TILES; ++x) {
+    col[x].l += sum[x];
+    Column::turn(p[x], p0[x], p1[x]);
+  }
   const float vs = tab.vs[EDGE ? min(SP * st + g, npg - 1) : SP * st + g];
   const uint8_t* vrow = in.v + g * PAGE + c * 16;
   if constexpr (!EDGE) {
