@@ -304,10 +304,17 @@ __device__ inline void token_block(const Args& a, const Tables& tab, const Token
 }
 
 // ---- chunks --------------------------------------------------------------------------------------------------
-// Bound by vector instructions beside the products: conversions and exponentials.  Each of the block's two wavefronts takes two
-// tiles, so that a page is widened once for 32 columns; the pages of a step lie once in LDS for both, as they lie in memory (every read
-// touches all banks: a page's K pieces are 1 KB in lane order, sixteen channels' V rows 256 bytes), and the next step's are on
-// their way meanwhile.
+// Bound by the card's power where launches follow each other, by vector instructions beside the products (conversions and
+// exponentials) in a launch of its own: 4096 new tokens over 40/8 heads (171 GFLOP) 200 - 216 us on several cards, 177 with codes and
+// queries of zeros.  Each of the block's two wavefronts takes two tiles as 32 columns; the pages of a step lie once in LDS for
+// both, as they lie in memory, and the next step's are on their way meanwhile.  v_mfma_f32_32x32x16_bf16:
+//   S^T[key, col]: A = two K pages, lane (r = lane % 32, h = lane / 32): channels 32 i + 16 h .. + 15, two products' worth, of the key in
+//                  slot (r with bits 2 and 3 exchanged) % 16 of page r / 16
+//   O^T[d, col]:   A = V rows of a page, lane (d = lane % 32, h): slots 8 h .. + 7, which with the exchange are the keys whose
+//                  scores a lane (col, h) has got: no word changes places
+// (The 16x16x32 form has the same rate, but every product takes 7 cycles of the vector instructions' time, and it needs twice as
+// many: two wavefronts of a SIMD spend 105 ns on eight of them with four conversions each, 76 on four of this form with eight each.  The
+// kernel in that form 204 us in a row of launches and 241 in one of its own, in this 200 and 223.)
 struct StepLds {
   uint8_t k[SP * PAGE], v[SP * PAGE];
 };
@@ -328,108 +335,152 @@ __device__ inline void load_step(const Args& a, const Tables& tab, StepLds& to, 
 }
 
 constexpr int TILES = FLEXCO_ATTN_ITEM_TILES / CHUNK_NW;      // of a wavefront
+static_assert(TILES == 2, "two tiles are a product's 32 columns");
 
-// EDGE: a key of the step may lie behind some column's position or the block's range (else no mask, no clearing).  pos: the columns' own
-// positions (-1: no column), end: one past the item's last, both relative to the block's key range
-template <bool EDGE>
-__device__ inline void chunk_step(float scale_log2, const Tables& tab, const StepLds& in, Column (&col)[TILES], int st, int npg,
-                                  const int (&pos)[TILES], int end, int lane) {
-  const int c = lane & 15, g = lane >> 4;
-  f32x4 acc[TILES][SP];
-#pragma unroll
-  for (int n = 0; n < SP; ++n) {
-    const float ks = tab.ks[EDGE ? min(SP * st + n, npg - 1) : SP * st + n];
-    bf16x8 kf[4];
-    widen(*reinterpret_cast<const u32x4*>(in.k + n * PAGE + lane * 16), ks, kf[0], kf[1]);
-    widen(*reinterpret_cast<const u32x4*>(in.k + n * PAGE + 1024 + lane * 16), ks, kf[2], kf[3]);
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) acc[x][n] = col[x].scores(kf);
-  }
-  const int k0 = SP * st * PS;
-  if constexpr (EDGE) {
-#pragma unroll
-    for (int x = 0; x < TILES; ++x)
-#pragma unroll
-      for (int n = 0; n < SP; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = k0 + n * PS + 4 * g + j;
-          if (key > pos[x] || key >= npg * PS) acc[x][n][j] = -INFINITY;
-        }
-  }
-  bf16x8 p0[TILES], p1[TILES];
-  f32x4 p[TILES][SP];
-  float sum[TILES];
-  bool more = false;
-#pragma unroll
-  for (int x = 0; x < TILES; ++x) {
-    sum[x] = col[x].exponentials(acc[x], scale_log2, p[x]);
-    more |= !(sum[x] <= MOST);
-  }
-  if (__builtin_amdgcn_ballot_w64(more) != 0)      // (one branch for all tiles)
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-      col[x].follow(acc[x], scale_log2);
-      sum[x] = col[x].exponentials(acc[x], scale_log2, p[x]);
-    }
-#pragma unroll
-  for (int x = 0; x < TILES; ++x) {
-    col[x].l += sum[x];
-    Column::turn(p[x], p0[x], p1[x]);
-  }
-  const float vs = tab.vs[EDGE ? min(SP * st + g, npg - 1) : SP * st + g];
-  const uint8_t* vrow = in.v + g * PAGE + c * 16;
-  if constexpr (!EDGE) {
-#pragma unroll
-    for (int mt = 0; mt < 8; ++mt) {
-      bf16x8 v0, v1;
-      widen(*reinterpret_cast<const u32x4*>(vrow + mt * 256), vs, v0, v1);
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) col[x].add(mt, v0, v1, p0[x], p1[x]);
-    }
-    return;
-  }
-  // slots behind the item's last position are cleared; NaN codes before it are taken out, and a product of their places with the
-  // places that a column sees says whose rows they belong in
-  const int left = min(end, npg * PS) - (k0 + g * PS);
-  uint32_t odd = 0;
-#pragma unroll
-  for (int mt = 0; mt < 8; ++mt) {
-    u32x4 w = *reinterpret_cast<const u32x4*>(vrow + mt * 256);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] &= first_bytes(left - 4 * i);
-      const uint32_t n = has_nan(w[i]);
-      odd |= n;
-      w[i] &= ~bytes_of(n, 0xffu);
-    }
-    bf16x8 v0, v1;
-    widen(w, vs, v0, v1);
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) col[x].add(mt, v0, v1, p0[x], p1[x]);
-  }
-  if (__builtin_amdgcn_ballot_w64(odd != 0) == 0) return;
-#pragma unroll
-  for (int x = 0; x < TILES; ++x) {
-    bf16x8 s0, s1;
+// Running state of a lane's column (col = lane % 32), half of its channels, the sums of its own keys.
+struct Wide {
+  bf16x8 q[8];        // channels 32 i + 16 h .. + 7, + 8 .. + 15
+  float m, l;
+  f32x16 o[4];        // d = 32 mt + 8 b + 4 h + j in 4 b + j
+
+  __device__ void start(const bf16_t* qr, int h, bool used) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      s0[i] = (bf16_t)(k0 + g * PS + i <= pos[x] ? 1.f : 0.f);
-      s1[i] = (bf16_t)(k0 + g * PS + 8 + i <= pos[x] ? 1.f : 0.f);
+      const u32x4 w = *reinterpret_cast<const u32x4*>(qr + (i >> 1) * 32 + h * 16 + (i & 1) * 8);
+      q[i] = __builtin_bit_cast(bf16x8, used ? w : u32x4{0, 0, 0, 0});       // (products of zeros draw less power)
     }
+    m = NO_KEY;
+    l = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < 8; ++mt) {
-      u32x4 w = *reinterpret_cast<const u32x4*>(vrow + mt * 256);
+    for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = bytes_of(has_nan(w[i] & first_bytes(left - 4 * i)), 0x38u);      // 1.0 where the code is NaN
-      bf16x8 v0, v1;
-      widen(w, 1.f, v0, v1);
-      f32x4 n = {0.f, 0.f, 0.f, 0.f};
-      n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, s0, n, 0, 0, 0);
-      n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, s1, n, 0, 0, 0);
+      for (int i = 0; i < 16; ++i) o[mt][i] = 0.f;
+  }
+  __device__ float exponentials(const f32x16 (&acc)[2], float scale_log2, f32x16 (&p)[2]) const {
+    float sum[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (n[j] > 0.f) col[x].o[mt][j] = __builtin_nanf("");
+    for (int n = 0; n < 8; ++n) {
+      const int x = n >> 2, i = 4 * (n & 3);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[x][i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[x][i + j], scale_log2, -m));
+      sum[n] = (p[x][i] + p[x][i + 1]) + (p[x][i + 2] + p[x][i + 3]);
+    }
+    return ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+  }
+  __device__ void follow(const f32x16 (&acc)[2], float scale_log2) {
+    float mx = acc[0][0];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, acc[x][i]);
+    const float m_new = fmaxf(m, max_xor32(mx) * scale_log2), alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[mt][i] *= alpha;
+  }
+};
+
+__device__ inline bf16x8 widen8(uint32_t w0, uint32_t w1, float s) {
+  const bf16x2 t[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w0, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w0, s, true),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w1, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w1, s, true)};
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { r[2 * i] = t[i][0]; r[2 * i + 1] = t[i][1]; }
+  return r;
+}
+
+// EDGE: a key of the step may lie behind some column's position or the block's range (else no mask, no clearing).  pos: the column's own
+// position (-1: no column), end: one past the item's last, both relative to the block's key range
+template <bool EDGE>
+__device__ inline void chunk_step(float scale_log2, const Tables& tab, const StepLds& in, Wide& col, int st, int npg, int pos, int end,
+                                  int lane) {
+  const int r = lane & 31, h = lane >> 5;
+  const int k0 = SP * st * PS;
+  f32x16 acc[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int n = 2 * x + (r >> 4);
+    const float ks = tab.ks[EDGE ? min(SP * st + n, npg - 1) : SP * st + n];
+    const uint8_t* krow = in.k + n * PAGE + h * 256 + ((r & 3) | (r & 4) << 1 | (r & 8) >> 1) * 16;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x8 lo, hi;
+      widen(*reinterpret_cast<const u32x4*>(krow + i * 512), ks, lo, hi);
+      acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, col.q[2 * i], acc[x], 0, 0, 0);
+      acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, col.q[2 * i + 1], acc[x], 0, 0, 0);
+    }
+  }
+  if constexpr (EDGE) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + (2 * x + (i >> 3)) * PS + 8 * h + (i & 7);
+        if (key > pos || key >= npg * PS) acc[x][i] = -INFINITY;
+      }
+  }
+  f32x16 p[2];
+  float sum = col.exponentials(acc, scale_log2, p);
+  if (__builtin_amdgcn_ballot_w64(!(sum <= MOST)) != 0) {
+    col.follow(acc, scale_log2);
+    sum = col.exponentials(acc, scale_log2, p);
+  }
+  col.l += sum;
+  bf16x8 pb[SP];
+#pragma unroll
+  for (int n = 0; n < SP; ++n)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pb[n][i] = (bf16_t)p[n >> 1][8 * (n & 1) + i];
+  // slots behind the item's last position are cleared; NaN codes before it are taken out, and a product of their places with the
+  // places that a column sees says whose rows they belong in
+  const uint8_t* vrow = in.v + r * 16 + h * 8;
+  const int limit = min(end, npg * PS) - k0 - 8 * h;
+  uint32_t odd = 0;
+#pragma unroll
+  for (int n = 0; n < SP; ++n) {
+    const float vs = tab.vs[EDGE ? min(SP * st + n, npg - 1) : SP * st + n];
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) {
+      u32x2 w = *reinterpret_cast<const u32x2*>(vrow + n * PAGE + mt * 512);
+      if constexpr (EDGE) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          w[i] &= first_bytes(limit - n * PS - 4 * i);
+          const uint32_t nan = has_nan(w[i]);
+          odd |= nan;
+          w[i] &= ~bytes_of(nan, 0xffu);
+        }
+      }
+      col.o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[0], w[1], vs), pb[n], col.o[mt], 0, 0, 0);
+    }
+  }
+  if constexpr (EDGE) {
+    if (__builtin_amdgcn_ballot_w64(odd != 0) == 0) return;
+    bf16x8 seen[SP];
+#pragma unroll
+    for (int n = 0; n < SP; ++n)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) seen[n][i] = (bf16_t)(k0 + n * PS + 8 * h + i <= pos ? 1.f : 0.f);
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) {
+      f32x16 hits;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) hits[i] = 0.f;
+#pragma unroll
+      for (int n = 0; n < SP; ++n) {
+        u32x2 w = *reinterpret_cast<const u32x2*>(vrow + n * PAGE + mt * 512);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = bytes_of(has_nan(w[i] & first_bytes(limit - n * PS - 4 * i)), 0x38u);   // 1.0 where the code is NaN
+        hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[0], w[1], 1.f), seen[n], hits, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (hits[i] > 0.f) col.o[mt][i] = __builtin_nanf("");
     }
   }
 }
@@ -493,21 +544,17 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
     return;
   }
   if constexpr (MODE != 1) {
-    const int group = a.nq / a.nkv, c = lane & 15, g = lane >> 4;
+    const int group = a.nq / a.nkv, c = lane & 15, x = (lane >> 4) & 1, h = lane >> 5;
     load_step(a, tab, ring0, 0, kvh, npg, wave, lane);
     keep_scales();
-    const int tiles = max(0, min(TILES, ntl - TILES * wave));      // (a wavefront without a tile only helps with the loads)
-    Column col[TILES];
-    int pos[TILES];
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-      const int tile = tile0 + (x < tiles ? TILES * wave + x : 0);
-      const int t0 = a.tile_tok0[tile], ntok = a.tile_ntok[tile];
-      const bool ok = x < tiles && c < ntok * group;
-      const int t = ok ? t0 + c / group : t0;
-      pos[x] = ok ? a.tok_pos[t] - pb * PS : -1;
-      col[x].start(a.q + (size_t)t * a.ldq + (size_t)(kvh * group + (ok ? c % group : 0)) * D, g);
-    }
+    const bool work = TILES * wave < ntl;                          // (a wavefront without a tile only helps with the loads)
+    const bool mine = TILES * wave + x < ntl;
+    const int tile = mine ? tile0 + TILES * wave + x : tile0, t0 = a.tile_tok0[tile];
+    const bool ok = mine && c < a.tile_ntok[tile] * group;
+    const int t = ok ? t0 + c / group : t0;
+    const int pos = ok ? a.tok_pos[t] - pb * PS : -1;
+    Wide col;
+    col.start(a.q + (size_t)t * a.ldq + (size_t)(kvh * group + (ok ? c % group : 0)) * D, h, ok);
     const int n_st = (npg + SP - 1) / SP;
     const int first = first_pos - pb * PS, end = last_pos + 1 - pb * PS;
     // my loads have landed and my reads of the buffer that is handed over have returned -> barrier -> everyone's have
@@ -519,7 +566,6 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
     asm volatile("" ::: "memory");            \
   }
     const float scale_log2 = a.scale_log2;
-    const bool work = tiles > 0;
     // first the steps that lie wholly before every column's own position, in pairs, then the rest
     int st = 0;
     for (const int n_free = (min(first + 1, npg * PS) / (SP * PS)) & ~1; st < n_free; st += 2) {
@@ -540,20 +586,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
       if (work) chunk_step<true>(scale_log2, tab, ring1, col, st + 1, npg, pos, end, lane);
     }
 #undef FLEXCO_KV8_HAND_OVER
+    const float lsum = sum_xor32(col.l);
+    if (!ok || split >= a.tile_nsplit[tile]) return;               // (the tile's own keys end before this split)
+    float row[64];
 #pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-      if (x >= tiles) break;
-      const int tile = tile0 + TILES * wave + x;
-      if (split >= a.tile_nsplit[tile]) continue;            // (the tile's own keys end before this split)
-      const float lsum = sum_xor32(sum_xor16(col[x].l));
-      if (c >= a.tile_ntok[tile] * group) continue;
-      float row[32];
-#pragma unroll
-      for (int mt = 0; mt < 8; ++mt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) row[4 * mt + j] = col[x].o[mt][j];
-      write_column(a, tile, split, 1, kvh, group, c, 4 * g, row, 8, 16, col[x].m, lsum, g == 0);
-    }
+    for (int i = 0; i < 64; ++i) row[i] = col.o[i >> 4][i & 15];
+    write_column(a, tile, split, 1, kvh, group, c, 4 * h, row, 16, 8, col.m, lsum, h == 0);
   }
 }
 
