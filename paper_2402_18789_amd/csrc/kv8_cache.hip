@@ -459,7 +459,7 @@ __device__ inline void append_any(const AppendArgs& a, const RopeFreq& freq, con
   }
 }
 
-// FORM 0: every run is one token, a block each.  Else a block per (run, kv head), runs of one token to the first head's; FORM 4, 8: pages of
+// FORM 0: every run is one token, a block each.  Else a block per (run, kv head), runs of one token to one of them; FORM 4, 8: pages of
 // sixteen, head_dim 16 FORM; 1: any.
 template <typename T, int FORM>
 __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeFreq freq, const T* qkv, T* q_out) {
@@ -467,11 +467,13 @@ __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeF
   const int run = FORM == 0 ? blockIdx.x : blockIdx.x / a.nkv, kvh = FORM == 0 ? 0 : blockIdx.x % a.nkv;
   const int t0 = a.runs[2 * run], n = a.runs[2 * run + 1];
   if (t0 < 0 || n < 1 || n > a.ps || t0 > a.T - n) return;              // (whole block, as below)
+  // (by turns: the blocks of one head all run on one part of the chip.  309 tokens beside 87 of chunks, 8 kv heads: 16.7 us there, 11.3 by turns.)
+  if (FORM != 0 && n == 1 && kvh != run % a.nkv) return;
   const int sl = a.slot[t0], page = sl / a.ps, at = sl % a.ps;
   if (sl < 0 || page >= a.num_pages || at + n > a.ps) return;
   uint32_t* amax = reinterpret_cast<uint32_t*>(cs + (FORM == 0 ? 1 : FORM == 1 ? GROUP : GROUP / 2) * a.d);
   if (n == 1) {
-    if (kvh == 0) append_token<T, FORM == 0 ? 2 : 0>(a, freq, qkv, q_out, t0, page, at, cs, amax);
+    append_token<T, FORM == 0 ? 2 : 0>(a, freq, qkv, q_out, t0, page, at, cs, amax);
   } else if constexpr (FORM >= 4) {
     append_page16<T, FORM>(a, freq, qkv, q_out, t0, n, kvh, page, at, reinterpret_cast<float*>(cs), amax);
   } else if constexpr (FORM == 1) {
