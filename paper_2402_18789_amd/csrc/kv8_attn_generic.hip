@@ -61,6 +61,18 @@ __global__ __launch_bounds__(64 * NW) void kv8_attn_generic_kernel(Kv8Args a, co
       const bool ok = j0 + lane < nk;
       const size_t ph = (size_t)bt[j / ps] * a.nkv + kvh;
       const uint8_t* kr = k_codes + ph * ps * d + (size_t)(j % ps) * 16;
+      const int n = min(64, nk - j0);
+      // sixteen keys of a channel: one page, one load (a run's are asked for before its scores, past the last key the last ones again)
+      u32x4 vw[4][DU];
+      if (ps % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = j0 + min(16 * i, (n - 1) & ~15);
+          const uint8_t* vr = v_codes + ((size_t)bt[k / ps] * a.nkv + kvh) * ps * d + k % ps;
+#pragma unroll
+          for (int u = 0; u < DU; ++u) vw[i][u] = *reinterpret_cast<const u32x4*>(vr + (size_t)min(lane + 64 * u, d - 1) * ps);   // (channels past head_dim: not stored)
+        }
+      }
       float s = 0.f;
 #pragma unroll 4
       for (int p = 0; p < pieces; ++p) {
@@ -82,20 +94,19 @@ __global__ __launch_bounds__(64 * NW) void kv8_attn_generic_kernel(Kv8Args a, co
       m = m_new;
       ps_w[lane] = p * v_scale[ph];
       __builtin_amdgcn_wave_barrier();
-      const int n = min(64, nk - j0);
 #pragma unroll
       for (int u = 0; u < DU; ++u) acc[u] *= alpha;
-      if (ps % 16 == 0) {                                     // sixteen keys of a channel: one page, one load
-        for (int g0 = 0; g0 < n; g0 += 16) {
-          const uint8_t* vr = v_codes + ((size_t)bt[(j0 + g0) / ps] * a.nkv + kvh) * ps * d + (j0 + g0) % ps;
-          const int gn = min(16, n - g0);
+      if (ps % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int gn = n - 16 * i;
+          if (gn <= 0) break;
 #pragma unroll
           for (int u = 0; u < DU; ++u) {
-            const int dd = min(lane + 64 * u, d - 1);         // (channels past head_dim: not stored)
             float v[16];
-            kv8_decode16(*reinterpret_cast<const u32x4*>(vr + (size_t)dd * ps), v);
+            kv8_decode16(vw[i][u], v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[u] += e < gn ? ps_w[g0 + e] * v[e] : 0.f;   // (slots past the last key may hold anything)
+            for (int e = 0; e < 16; ++e) acc[u] += e < gn ? ps_w[16 * i + e] * v[e] : 0.f;   // (slots past the last key may hold anything)
           }
         }
       } else {
