@@ -40,6 +40,7 @@ struct Args {
   const int32_t *tok_pos, *block_table, *tile_req, *tile_tok0, *tile_ntok, *tile_nsplit, *tile_part0, *item_tile,
       *item_split, *item_ntiles, *req_tok_off;
   int max_pages, nq, nkv, n_items, split_pages, fold;
+  bool whole;         // fold holds for every request, not for those of one token alone
   float scale_log2;   // log2(e) / sqrt(d)
   const bf16_t* q;
   size_t ldq;
@@ -505,7 +506,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
   const int tok_last = a.tile_tok0[tl] + a.tile_ntok[tl] - 1;
   const bool lone = ntl == 1 && ntok_first == 1;
   // (a chunk's odd last token is a single token too, but keeps the key ranges of its request)
-  const int fold = a.fold > 1 && a.req_tok_off[r + 1] - a.req_tok_off[r] == 1 ? a.fold : 1;
+  const int fold = a.fold > 1 && (a.whole || a.req_tok_off[r + 1] - a.req_tok_off[r] == 1) ? a.fold : 1;
   if (split % fold != 0) return;                           // the block of an earlier split takes this one's keys (whole block)
   const int pb = split * a.split_pages;
   // The block's start is a chain of lookups in front of its first codes: each step asks for all it can.  The page ids of the range, and
@@ -591,7 +592,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
     float row[64];
 #pragma unroll
     for (int i = 0; i < 64; ++i) row[i] = col.o[i >> 4][i & 15];
-    write_column(a, tile, split, 1, kvh, group, c, 4 * h, row, 16, 8, col.m, lsum, h == 0);
+    write_column(a, tile, split, fold, kvh, group, c, 4 * h, row, 16, 8, col.m, lsum, h == 0);
   }
 }
 
@@ -681,7 +682,7 @@ int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& 
   a.tile_ntok = m.tile_ntok; a.tile_nsplit = m.tile_nsplit; a.tile_part0 = m.tile_part0; a.item_tile = m.item_tile;
   a.item_split = m.item_split; a.item_ntiles = m.item_ntiles; a.req_tok_off = m.req_tok_off;
   a.max_pages = m.max_pages; a.nq = c.n_q_heads; a.nkv = c.n_kv_heads; a.n_items = m.n_items; a.split_pages = m.kv_split_pages;
-  a.fold = fold;
+  a.fold = fold; a.whole = plan.whole;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   a.q = (const bf16_t*)q; a.ldq = ldq;
   a.k_codes = pool.k_codes; a.v_codes = pool.v_codes; a.k_scale = pool.k_scale; a.v_scale = pool.v_scale;
@@ -703,7 +704,7 @@ int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FLEXCO_EHIP, "launch of kv8_attn failed: %s", hipGetErrorString(e));
   // every request in one piece: nothing to join
-  if (m.n_parts == m.n_tiles || (m.n_single == m.n_items && m.max_pages <= fold * m.kv_split_pages)) return FLEXCO_OK;
+  if (m.n_parts == m.n_tiles || plan.whole || (m.n_single == m.n_items && m.max_pages <= fold * m.kv_split_pages)) return FLEXCO_OK;
   KernelTimerScope ts(FLEXCO_K_ATTN_MERGE, s);
   // The long form from nine pieces on where there are few rows (4 tokens of 4000 keys in eights 18.4 -> 15.1 us, 8 of 8000 in 32s 36.0 -> 32.5;
   // with 256 x 16 rows of up to five pieces it cost 4 more), from seventeen on in any case.
