@@ -2,7 +2,8 @@
 //
 // Append.  A page's scale is chosen from all of its new rows, so the rotated keys and the values of a (run, kv head) are held until
 // their largest magnitude is known; whoever does that owns the page's codes of the head, so a scale that has grown is applied to the
-// codes already there on the spot.  Bound by HBM: (2 nq + 2 nkv) d activations and 2 nkv d bytes per token.
+// codes already there on the spot.  Bound by HBM for many tokens: (2 nq + 2 nkv) d activations and 2 nkv d bytes per token (4000 tokens of chunks over
+// 32/8 heads 21.5 us, 4.2 TB/s), by latency for few (one 6.1 us, 512 single ones over 40/8 heads 9.5).
 // Keys are rotated in double precision and rounded once, into the cache (an angle's fp32 error of 5e-7 moved one code in 10^5).
 #include "flexco_internal.h"
 #include "flexco_kv8.h"
@@ -481,7 +482,8 @@ __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeF
   }
 }
 
-// Expand.  One block per (page, kv head): 2 d ps codes in, as many elements out.
+// Expand.  One block per (page, kv head): 2 d ps codes in, as many elements out, keys beside values so that a page of 16 x 128 is one unit of
+// sixteen codes a thread.  Bound by HBM: 32749 tokens of 8 x 128 to bf16 46 us, 4.3 TB/s; 2048 tokens 5.1 us, a launch's time.
 template <typename T>
 __global__ __launch_bounds__(THREADS) void kv8_expand_kernel(const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ v_codes,
                                                              const float* __restrict__ k_scale, const float* __restrict__ v_scale,
