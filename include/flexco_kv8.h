@@ -43,7 +43,7 @@ typedef struct flexco_kv8_pool {
 /* The runs of a batch: its tokens by the page they are written to (one scale is chosen per run and head).  host_maps: as filled by
  * flexco_build_maps, arrays in host memory.  runs (host): pairs (first token, number of tokens), batch order, room for
  * `capacity` pairs (host_maps->T always suffices); *n_runs = pairs written.  Host only.
- * Errors: EINVAL, EPAGE (two runs write into one page: its scale would be chosen twice), EWORKSPACE (capacity). */
+ * Errors: EINVAL, EPAGE (two runs write into one page: its scale would be chosen twice), EWORKSPACE (capacity, or no host memory). */
 int32_t flexco_kv8_runs(const flexco_maps* host_maps, int32_t* runs, int32_t capacity, int32_t* n_runs);
 
 /* Append of the batch's tokens (Alg. 2: Append): queries and keys are rotated to their positions, keys and values written to
@@ -77,8 +77,8 @@ int32_t flexco_kv8_attention(const flexco_layer_cfg* cfg, const flexco_maps* map
 int32_t flexco_kv8_expand(const flexco_layer_cfg* cfg, const flexco_kv8_pool* pool, const int32_t* src_pages, int32_t n_tokens,
                           const flexco_kv_pool* wide, const int32_t* dst_pages, void* stream);
 
-/* flexco_layer_forward over an 8-bit pool: flexco_kv8_append and flexco_kv8_attention in place of the 16-bit steps, everything else -
- * arguments, the finetune window's saved rows, workspace - as there.  A later flexco_lora_bwd of the window takes a pool that
+/* flexco_layer_forward over an 8-bit pool: flexco_kv8_append (of all the batch's runs) and flexco_kv8_attention in place of the 16-bit
+ * steps, everything else - arguments, the finetune window's saved rows, workspace - as there.  A later flexco_lora_bwd of the window takes a pool that
  * flexco_kv8_expand has filled with the sequence's pages. */
 int32_t flexco_kv8_layer_forward(const flexco_layer_cfg* cfg, const flexco_base_weights* w, const flexco_lora* lora,
                                  const flexco_maps* maps, const int32_t* runs, int32_t n_runs, const void* x_in, void* x_out,

@@ -1,4 +1,5 @@
 // Host side of the 8-bit cache: which tokens of a batch share a page.  No device calls.
+#include <new>
 #include <unordered_set>
 
 #include "flexco_host.h"
@@ -8,8 +9,8 @@ using namespace flexco;
 
 extern "C" int32_t flexco_kv8_abi_version(void) { return 1; }
 
-extern "C" int32_t flexco_kv8_runs(const flexco_maps* host_maps, int32_t* runs, int32_t capacity, int32_t* n_runs) {
-  clear_error();
+namespace {
+int32_t find_runs(const flexco_maps* host_maps, int32_t* runs, int32_t capacity, int32_t* n_runs) {
   FLEXCO_CHECK(host_maps && runs && n_runs, FLEXCO_EINVAL, "NULL argument");
   FLEXCO_CHECK(capacity >= 0, FLEXCO_EINVAL, "negative capacity");
   const flexco_maps& m = *host_maps;
@@ -33,4 +34,14 @@ extern "C" int32_t flexco_kv8_runs(const flexco_maps* host_maps, int32_t* runs, 
   }
   *n_runs = n;
   return FLEXCO_OK;
+}
+}  // namespace
+
+extern "C" int32_t flexco_kv8_runs(const flexco_maps* host_maps, int32_t* runs, int32_t capacity, int32_t* n_runs) {
+  clear_error();
+  try {
+    return find_runs(host_maps, runs, capacity, n_runs);
+  } catch (const std::bad_alloc&) {                          // (no exception passes the C boundary)
+    return fail(FLEXCO_EWORKSPACE, "no host memory for the batch's pages");
+  }
 }

@@ -245,3 +245,24 @@ def test_a_page_is_read_for_two():
     assert torch.equal(wide.k[0], wide.k[3]) and torch.equal(wide.v[0], wide.v[3]) and not wide.k[2].any()
     codes, scale = from_device(pool)
     assert np.array_equal(to_np(wide.v[1]), (O8.decode(codes["v"][1]) * 2.0).transpose(1, 2, 0))
+
+
+def test_append_and_pages_written_out_past_4_gib():
+    """pages whose codes, and whose elements in the wide pool, lie beyond 2^32 bytes: what pages at the front get"""
+    cfg = shape(32, 16)
+    first, wide_first = (1 << 32) // (16 * 16 * 128), (1 << 32) // (16 * 16 * 128 * 2)
+    reqs, pages, n = make_batch(cfg, [(D, 33, 1), (P, 5, 50), (D, 16, 1)])
+    x = device(gen.rng(0, "kv8", "x").standard_normal((52, cfg.qkv_dim)), cfg)
+    c, got = HH.c_cfg(cfg), []
+    for at, wide_at in ((0, 0), (first, wide_first)):
+        pool, wide = kv8.DevicePool8(cfg, at + n), HH.DevicePool(cfg, wide_at + 4)
+        db = kv8.DeviceBatch8(cfg, reqs, {i: p + np.int32(at) for i, p in pages.items()}, at + n)
+        q = torch.empty((52, cfg.q_dim), dtype=x.dtype, device="cuda")
+        kv8.flexco_kv8_append(c, db.maps, db.runs, db.n_runs, x, pool.c, q, cfg.q_dim)
+        src = torch.from_numpy(pages[1] + np.int32(at)).cuda()
+        pool.expand(src, 55, wide, torch.arange(wide_at, wide_at + 4, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        got.append([t.clone() for t in (q, pool.k[at:], pool.v[at:], pool.k_scale[at:], pool.v_scale[at:], wide.k[wide_at:], wide.v[wide_at:])])
+        assert not pool.k[:at].any() and not wide.v[:wide_at].any()
+        del pool, wide
+    assert all(torch.equal(a, b) for a, b in zip(*got))
