@@ -116,6 +116,29 @@ def test_some_of_a_batchs_runs():
     assert not some.k[others].any() and not some.v[others].any() and not some.k_scale[others].any()
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("cfg", [shape(40, 8), shape(4, 4, 64, "f32")], ids=lambda c: c.name)
+def test_single_tokens_in_any_order_of_runs(cfg, in_place):
+    """as many runs as tokens, in the batch's order and in others: the same pages, scales and queries"""
+    n = 37
+    reqs, pages, num_pages = make_batch(cfg, [(D, int(v), 1) for v in gen.rng(4, "kv8", "pos").integers(0, 90, n)])
+    cache = O8.Cache8(num_pages, cfg.page_size, cfg.n_kv_heads, cfg.head_dim)
+    fill_prefixes(cfg, cache, reqs, pages, 0)
+    db = kv8.DeviceBatch8(cfg, reqs, pages, num_pages)
+    assert db.n_runs == db.host_maps.T == n
+    c, got = HH.c_cfg(cfg), []
+    x = device(gen.rng(0, "kv8", "x").standard_normal((n, cfg.qkv_dim)), cfg)
+    for order in (np.arange(n), np.arange(n)[::-1], gen.rng(5, "kv8", "order").permutation(n)):
+        pool, rows = to_device(cfg, cache, num_pages), x.clone()
+        q, ld = (rows, cfg.qkv_dim) if in_place else (torch.zeros((n, cfg.q_dim), dtype=x.dtype, device="cuda"), cfg.q_dim)
+        runs = torch.from_numpy(np.ascontiguousarray(db.host_runs[order])).cuda()
+        kv8.flexco_kv8_append(c, db.maps, runs, n, rows, pool.c, q, ld)
+        torch.cuda.synchronize()
+        got.append((q, pool.k, pool.v, pool.k_scale, pool.v_scale))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
 @pytest.mark.parametrize("cfg", [shape(8, 2), shape(4, 2, 64, "f32")], ids=lambda c: c.name)
 def test_sequences_that_share_their_prefix(cfg):
     """three sequences whose first pages are the same ones, each with a page of its own behind: the rows of copies in pages of their own"""
