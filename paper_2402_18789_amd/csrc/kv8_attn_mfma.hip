@@ -3,7 +3,7 @@
 //
 // A column is a (token, query head) pair, a tile sixteen of them over one kv head.  Codes are widened to bf16 in registers, by
 // conversions that multiply by their page's scale on the way, a power of two: code x scale is a bf16 number, so nothing is rounded there,
-// and from then on the products are those of a 16-bit cache (v_mfma_f32_16x16x32_bf16):
+// and from then on the products are those of a 16-bit cache.  Single tokens (v_mfma_f32_16x16x32_bf16; chunks: below):
 //   S^T[key, col] = K[key, :] . Q[col, :]^T         A = a K page (16 keys), lane (key, g): channels 16 g .. + 15 and 64 + 16 g .. + 15
 //   O^T[d, col] += V^T[d, keys] . P^T[keys, col]    A = V rows as they lie, lane (d = lane % 16, g): the 16 keys of the g-th of four pages
 // (The 8-bit products of the chip, with the other operand as the sum of two e4m3 numbers, need no conversion and were tried first:
