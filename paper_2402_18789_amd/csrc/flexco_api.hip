@@ -786,8 +786,7 @@ int32_t run_kv8_attention(const flexco_layer_cfg& c, const flexco_maps& m, const
     FLEXCO_TRY(launch_kv8_attention_generic(c, m, q, ldq, pool, part_ml, part_acc, out, ldo, lse, s, keep));
   }
   if (m.n_parts == m.n_tiles) return FLEXCO_OK;
-  KernelTimerScope ts(FLEXCO_K_ATTN_MERGE, s);
-  return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, 1, keep);
+  return launch_kv8_merge(c, m, part_ml, part_acc, out, ldo, lse, s, 1, keep);
 }
 
 }  // namespace

@@ -596,77 +596,6 @@ __global__ __launch_bounds__(64 * NW, 2) void kv8_attn_kernel(Args a) {
   }
 }
 
-// ---- joining the partial rows of a long axis ---------------------------------------------------------------
-// A block per (token, query head), for lists in which a request is cut into many pieces: eight groups of 32 lanes take the pieces in
-// turn, four loads at a time, and add up in LDS in group order.  (The merge that lists of few pieces take walks them one group per row:
-// 118 pieces of three long contexts 50 us.)
-constexpr int MG = 8;
-__global__ __launch_bounds__(32 * MG) void kv8_merge_long_kernel(Args a, const int32_t* __restrict__ tok_tile, const int32_t* __restrict__ tok_req) {
-  __shared__ float red_m[32 * MG / 64], part[MG][D], part_l[MG];
-  const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, grp = tid >> 5, ln = tid & 31;
-  const int group = a.nq / a.nkv, kvh = h / group, tile = tok_tile[t], r = tok_req[t];
-  const int fold = a.fold > 1 && a.req_tok_off[r + 1] - a.req_tok_off[r] == 1 ? a.fold : 1;
-  const int n = (a.tile_nsplit[tile] + fold - 1) / fold;       // partial rows
-  if (n == 1) return;                                          // the attention kernel has written these rows itself (whole block)
-  const int cpt = (16 / group > 1 ? 16 / group : 1) * group;
-  const size_t idx0 = ((size_t)a.tile_part0[tile] * a.nkv + kvh) * cpt + (t - a.tile_tok0[tile]) * group + h % group;
-  const size_t step = (size_t)fold * a.nkv * cpt;
-  float m = -INFINITY;
-  for (int i = tid; i < n; i += 32 * MG) m = fmaxf(m, a.part_ml[(idx0 + i * step) * 2]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if ((tid & 63) == 0) red_m[tid >> 6] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 32 * MG / 64; ++w) m = fmaxf(m, red_m[w]);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  constexpr int U = 4;
-  for (int i0 = grp; i0 < n; i0 += MG * U) {
-    float2 ml[U];
-    f32x4 v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const size_t idx = idx0 + min(i0 + u * MG, n - 1) * step;
-      ml[u] = *reinterpret_cast<const float2*>(a.part_ml + idx * 2);
-      v[u] = *reinterpret_cast<const f32x4*>(a.part_acc + idx * D + 4 * ln);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + u * MG < n && !(ml[u].x == -INFINITY)) {       // (the sums of a piece without a visible key are not written)
-        const float w = __expf(ml[u].x - m);
-        l += ml[u].y * w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] += v[u][j] * w;
-      }
-  }
-  *reinterpret_cast<f32x4*>(&part[grp][4 * ln]) = acc;
-  if (ln == 0) part_l[grp] = l;
-  __syncthreads();
-  if (grp != 0) return;
-  f32x4 row = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.f;
-#pragma unroll
-  for (int w = 0; w < MG; ++w) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(&part[w][4 * ln]);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) row[j] += v[j];
-    L += part_l[w];
-  }
-  const float inv = 1.0f / L;
-  bf16x4 o;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) o[j] = (bf16_t)(row[j] * inv);
-  const bool kept = a.keep.lse2 && t >= a.keep.tok0 && t < a.keep.tok0 + a.keep.n;
-  *reinterpret_cast<bf16x4*>(a.out + (size_t)t * a.ldo + h * D + 4 * ln) = o;
-  if (kept) *reinterpret_cast<bf16x4*>((bf16_t*)a.keep.out2 + ((size_t)(t - a.keep.tok0) * a.nq + h) * D + 4 * ln) = o;
-  if (ln == 0) {
-    const float z = m + __logf(L);
-    if (a.lse) a.lse[(size_t)t * a.nq + h] = z;
-    if (kept) a.keep.lse2[(size_t)(t - a.keep.tok0) * a.nq + h] = z;
-  }
-}
-
 }  // namespace
 
 int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& m, const void* q, size_t ldq, const flexco_kv8_pool& pool,
@@ -705,17 +634,7 @@ int32_t launch_kv8_attention_mfma(const flexco_layer_cfg& c, const flexco_maps& 
   if (e != hipSuccess) return fail(FLEXCO_EHIP, "launch of kv8_attn failed: %s", hipGetErrorString(e));
   // every request in one piece: nothing to join
   if (m.n_parts == m.n_tiles || plan.whole || (m.n_single == m.n_items && m.max_pages <= fold * m.kv_split_pages)) return FLEXCO_OK;
-  KernelTimerScope ts(FLEXCO_K_ATTN_MERGE, s);
-  // The long form from nine pieces on where there are few rows (4 tokens of 4000 keys in eights 18.4 -> 15.1 us, 8 of 8000 in 32s 36.0 -> 32.5;
-  // with 256 x 16 rows of up to five pieces it cost 4 more), from seventeen on in any case.
-  const int most = (m.max_pages + fold * m.kv_split_pages - 1) / (fold * m.kv_split_pages);
-  const bool long_axis = most > 16 || (most > 8 && (int64_t)m.T * c.n_q_heads <= 2048);
-  if (!long_axis)
-    return launch_attention_merge(c, m, part_ml, part_acc, out, ldo, lse, s, fold, keep);
-  hipLaunchKernelGGL(kv8_merge_long_kernel, dim3(m.T, c.n_q_heads), dim3(32 * MG), 0, s, a, m.tok_tile, m.tok_req);
-  e = hipGetLastError();
-  if (e != hipSuccess) return fail(FLEXCO_EHIP, "launch of kv8_merge_long failed: %s", hipGetErrorString(e));
-  return FLEXCO_OK;
+  return launch_kv8_merge(c, m, part_ml, part_acc, out, ldo, lse, s, fold, keep);
 }
 
 }  // namespace flexco

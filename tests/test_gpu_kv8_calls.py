@@ -60,6 +60,16 @@ def test_pieces_beside_chunks(cfg):
     check_attention(cfg, reqs, rows_of=(0, 1, 31))
 
 
+@pytest.mark.parametrize("cfg", [shape(4, 2, 64, "f32"), shape(6, 3, 48), shape(16, 2, 256), shape(2, 1, 16, "f32"), shape(34, 2), shape(4, 2, 128, "bf16", 5)],
+                         ids=lambda c: c.name)
+def test_many_pieces_of_other_shapes(cfg):
+    reqs = [(D, 5000, 1), (D, 3, 1), (P, 2100, 20)]
+    _, m = plan_of(cfg, reqs)
+    assert -(-m.max_pages // m.kv_split_pages) > 16
+    check_attention(cfg, reqs, rows_of=(0, 7))
+    check_attention(cfg, reqs, rows_of=(0, 7), split=16, use_lse=False)
+
+
 # Scores that grow from page to page (every step moves the reference of the exponentials), shrink, or jump both ways.
 @pytest.mark.parametrize("law", [lambda j: j, lambda j: -j, lambda j: (j * 7) % 11, lambda j: 8 * (j % 5 == 4)])
 @pytest.mark.parametrize("cfg", [shape(8, 2), shape(4, 2, 64, "f32")], ids=lambda c: c.name)
