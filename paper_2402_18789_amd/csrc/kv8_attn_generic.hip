@@ -8,6 +8,7 @@
 // are.  Only keys up to the column's own position are read.  Bound by the latency of a run's loads, sums and exchanges: about 3 us
 // per 64 keys of a wavefront, 8.1 us for 4 requests and two chunks of up to 64 keys (fp32, 4 heads of 64).
 #include <algorithm>
+#include <cfloat>
 #include "flexco_internal.h"
 #include "kv8_codes.h"
 #include "kv8_internal.h"
@@ -135,7 +136,8 @@ __global__ __launch_bounds__(64 * NW) void kv8_attn_generic_kernel(Kv8Args a, co
       if (kept) st((T*)a.keep.out2 + ((size_t)(t - a.keep.tok0) * a.nq + h) * d + dd, acc[u] * inv);
     }
     if (lane == 0) {
-      if (!whole) { part_ml[idx * 2] = m; part_ml[idx * 2 + 1] = l; }
+      // (-infinity: no visible key, left out by the join.  Keys of NaN scores alone leave m there too, and their NaN has to get past it.)
+      if (!whole) { part_ml[idx * 2] = l == l ? m : fmaxf(m, -FLT_MAX); part_ml[idx * 2 + 1] = l; }
       else if (a.lse) a.lse[(size_t)t * a.nq + h] = m + __logf(l);
       if (kept) a.keep.lse2[(size_t)(t - a.keep.tok0) * a.nq + h] = m + __logf(l);
     }

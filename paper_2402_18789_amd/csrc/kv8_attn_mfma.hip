@@ -153,7 +153,8 @@ struct Column {
 __device__ inline void write_column(const Args& a, int tile, int split, int fold, int kvh, int group, int c, int dd, const float* row4,
                                     int n4, int stride, float m, float lsum, bool first) {
   const int cpt = (16 / group > 1 ? 16 / group : 1) * group;
-  const float mn = m == NO_KEY ? -INFINITY : m * 0.6931471805599453f;
+  // (a piece without a visible key is one whose sum is zero: NaN scores leave m where it was too, and their NaN has to get past the join)
+  const float mn = m == NO_KEY && lsum == 0.f ? -INFINITY : m * 0.6931471805599453f;
   if (a.tile_nsplit[tile] <= fold) {
     const int t = a.tile_tok0[tile] + c / group, h = kvh * group + c % group;
     const float inv = 1.0f / lsum;

@@ -1,5 +1,6 @@
 // Joining the partial rows of the 8-bit attention: a row's pieces are (m_i, l_i, o_i), sums of exp(s - m_i) and of exp(s - m_i) v over the keys
 // of a piece; with M = max m_i the row is sum o_i exp(m_i - M) / sum l_i exp(m_i - M), its log-sum-exp M plus the log of that sum.
+// A piece without a visible key has m_i = -infinity and is left out; one whose keys' scores are all NaN has the lowest finite m_i.
 #include "device_types.h"
 #include "flexco_internal.h"
 #include "kv8_internal.h"

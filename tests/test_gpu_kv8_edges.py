@@ -1,0 +1,59 @@
+"""The 8-bit cache where its rules meet each other.  Bounds are those of test_gpu_kv8.py unless a test says otherwise."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_common import to_np
+from kv8_plan import kv8_plan, pieces
+from oracle import kv8 as O8
+from oracle import layer as OL
+from oracle.maps import build_maps
+from paper_2402_18789_amd import host as HH
+from paper_2402_18789_amd import kv8
+from test_gpu_kv8 import C1, C2, D, F, P, check_append, check_attention, device, fill_prefixes, from_device, half_step, make_batch, say, shape, to_device
+from workload import gen
+from workload.configs import KIND_FINETUNE
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- NaN keys in a piece of their own -----------------------------------------------------------------------
+
+# Bf16 of head_dim 128: a request of one token of 1025 or 4097 keys is cut into pieces of 16 pages (asserted below), the last of them one
+# key.  Other shapes and chunks: pieces of `split` pages.  In each case the requests' keys in `odd` are NaN, in one channel of the last kv head.
+BF16, F32, F32W = shape(8, 2), shape(4, 2, 64, "f32"), shape(4, 2, 128, "f32")
+CUT = [
+    # the last key of a single token, the first of a chunk's last piece, a chunk's piece in the middle: merged a group of lanes per row
+    (BF16, 2, [(D, 1024, 1), (P, 96, 20), (F, 64, 70), (D, 40, 1)], {0: [(1024, 1025)], 1: [(96, 97)], 2: [(32, 64)]}, 5),
+    (BF16, 0, [(D, 1024, 1)], {0: [(1024, 1025)]}, 5),
+    (BF16, 0, [(D, 1024, 1), (D, 900, 1)], {0: [(256, 512)], 1: [(0, 256)]}, 5),
+    (BF16, 8, [(P, 512, 40), (P, 0, 300)], {0: [(512, 513)], 1: [(128, 256)]}, None),
+    # by a block per row
+    (BF16, 2, [(D, 4096, 1)], {0: [(4096, 4097)]}, 17),
+    (BF16, 2, [(D, 4096, 1), (P, 96, 20)], {0: [(1024, 1280)], 1: [(64, 96)]}, 17),
+    # other shapes: a wavefront per row, a group of lanes, a block
+    (F32, 2, [(D, 64, 1), (P, 96, 20), (F, 64, 70)], {0: [(64, 65)], 1: [(96, 97)], 2: [(32, 64)]}, None),
+    (F32, 8, [(D, 384, 1), (P, 0, 200)], {0: [(128, 256)], 1: [(128, 129)]}, None),
+    (F32W, 2, [(D, 64, 1), (P, 96, 20)], {0: [(64, 65)], 1: [(32, 64)]}, None),
+    (F32, 2, [(D, 1024, 1), (P, 96, 20)], {0: [(1024, 1025)], 1: [(96, 97)]}, None),
+    (shape(34, 2), 2, [(D, 1024, 1), (P, 96, 20)], {0: [(512, 544)], 1: [(96, 97)]}, None),
+]
+
+
+@pytest.mark.parametrize("cfg,split,reqs,odd,n_pieces", CUT, ids=lambda v: getattr(v, "name", None))
+def test_nan_keys_alone_in_a_piece_show(cfg, split, reqs, odd, n_pieces):
+    """a row that sees a NaN key is NaN and so is its log-sum-exp, however its context is cut; other heads and rows are what they are"""
+    batch, pages, num_pages = make_batch(cfg, reqs)
+    m = kv8.DeviceBatch8(cfg, batch, pages, num_pages, split, device=None).host_maps
+    if n_pieces:
+        assert pieces(m, kv8_plan(m, cfg.n_kv_heads)) == n_pieces
+    else:
+        assert m.n_parts > m.n_tiles
+
+    def edit(cache, requests, pages_of):
+        for i, ranges in odd.items():
+            for lo, hi in ranges:
+                for at in range(lo, hi):
+                    cache.codes["k"][pages_of[i][at // 16], at % 16, cfg.n_kv_heads - 1, 5] = 0x7F
+
+    check_attention(cfg, reqs, split=split, edit=edit, rows_of=(0, 1, 30, 69, 127, 128, 255, 256))
