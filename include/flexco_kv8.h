@@ -49,7 +49,7 @@ int32_t flexco_kv8_runs(const flexco_maps* host_maps, int32_t* runs, int32_t cap
 /* Append of the batch's tokens (Alg. 2: Append): queries and keys are rotated to their positions, keys and values written to
  * their slots.
  *   maps  : device-rebased maps of the batch;  runs: device, the n_runs pairs of flexco_kv8_runs for these maps (a run
- *           outside the batch or reaching past its page is left out)
+ *           outside the batch, e.g. (-1, 0) in a place left free, or reaching past its page is left out)
  *   qkv   : device [T, (nq + 2 nkv) d], rows of query, key and value heads before rotation, dtype of cfg
  *   q_out : device, T rows of nq d elements, ld_q elements apart: the rotated queries.  q_out may be qkv with ld_q its row length
  *           (rotation in place; keys and values are left as they are); else the two may not overlap.

@@ -470,7 +470,7 @@ __device__ inline void append_any(const AppendArgs& a, const RopeFreq& freq, con
   }
 }
 
-// FORM 0: every run is one token, a block each.  Else a block per (run, kv head), runs of one token to one of them; FORM 4, 8: pages of
+// FORM 0: every run is one token or outside the batch, a block each.  Else a block per (run, kv head), runs of one token to one of them; FORM 4, 8: pages of
 // sixteen, head_dim 16 FORM; 1: any.
 template <typename T, int FORM>
 __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeFreq freq, const T* qkv, T* q_out) {
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeF
   constexpr int QP = FORM == 0 ? 2 : 0;
   TokenRow<T, QP> held;
   int sl = 0, pos = 0;
-  // (as many runs as tokens: run i is token i unless the caller has put them in an order of their own, so that its row, slot and position are asked
+  // (a single token each and as many runs: run i is token i unless the caller has put them in an order of their own, so that its row, slot and position are asked
   // for along with the run itself: one token, a launch of its own 7.8 -> 7.2 us, 512 11.6 -> 11.2)
   if (FORM == 0) {
     held.load(a, row_of(a, qkv, run));
@@ -562,7 +562,10 @@ int32_t launch_kv8_append(const flexco_layer_cfg& c, const flexco_maps& m, const
   FLEXCO_TRY(rope_freq(c, &freq));
   const AppendArgs a{runs, m.tok_pos, m.slot, pool.k_codes, pool.v_codes, pool.k_scale, pool.v_scale, n_runs, m.T, pool.num_pages,
                      pool.page_size, c.n_q_heads, c.n_kv_heads, c.head_dim, ld_q, m.ft_tok0, q_cache ? m.n_ft : 0, q_cache};
-  const int form = n_runs == m.T ? 0 : c.page_size == 16 && c.head_dim == 128 ? 8 : c.page_size == 16 && c.head_dim == 64 ? 4 : 1;
+  // (as many runs as tokens are not enough for form 0, which takes single tokens alone: places of a list may be free, runs outside the batch.  A token
+  // per request, or per page, is.)
+  const bool single_tokens = n_runs == m.T && (m.n_req == m.T || c.page_size == 1);
+  const int form = single_tokens ? 0 : c.page_size == 16 && c.head_dim == 128 ? 8 : c.page_size == 16 && c.head_dim == 64 ? 4 : 1;
   const dim3 grid(form == 0 ? (unsigned)n_runs : (unsigned)n_runs * c.n_kv_heads);
   const size_t shm = sizeof(double) * (form == 0 ? 1 : form == 1 ? GROUP : GROUP / 2) * c.head_dim +
                      (4 * sizeof(uint32_t) + c.head_dim) * c.n_kv_heads;

@@ -57,3 +57,32 @@ def test_nan_keys_alone_in_a_piece_show(cfg, split, reqs, odd, n_pieces):
                     cache.codes["k"][pages_of[i][at // 16], at % 16, cfg.n_kv_heads - 1, 5] = 0x7F
 
     check_attention(cfg, reqs, split=split, edit=edit, rows_of=(0, 1, 30, 69, 127, 128, 255, 256))
+
+
+# ---- runs ---------------------------------------------------------------------------------------------------
+
+def appended(cfg, db, num_pages, cache, x, runs):
+    pool, q = to_device(cfg, cache, num_pages), torch.full((db.host_maps.T, cfg.q_dim), 7.0, dtype=x.dtype, device="cuda")
+    runs = torch.from_numpy(np.ascontiguousarray(runs, dtype=np.int32)).cuda()
+    kv8.flexco_kv8_append(HH.c_cfg(cfg), db.maps, runs, len(runs), x, pool.c, q, cfg.q_dim)
+    torch.cuda.synchronize()
+    return q, pool.k, pool.v, pool.k_scale, pool.v_scale
+
+
+@pytest.mark.parametrize("cfg", [shape(), shape(40, 8), shape(4, 4, 64, "f32"), shape(6, 3, 48), shape(4, 2, 128, "bf16", 5)], ids=lambda c: c.name)
+@pytest.mark.parametrize("reqs_in", [[(D, 33, 1), (P, 5, 50)], [(F, 9, 70)], [(D, 33, 1), (P, 0, 2)], [(D, 7, 1), (D, 16, 1), (D, 0, 1)]], ids=str)
+def test_runs_with_places_left_free(cfg, reqs_in):
+    """a list as long as the batch, its places behind the runs (or between them) filled with runs outside the batch: what the runs alone give"""
+    reqs, pages, num_pages = make_batch(cfg, reqs_in)
+    cache = O8.Cache8(num_pages, cfg.page_size, cfg.n_kv_heads, cfg.head_dim)
+    fill_prefixes(cfg, cache, reqs, pages, 0)
+    db = kv8.DeviceBatch8(cfg, reqs, pages, num_pages)
+    T = db.host_maps.T
+    x = device(gen.rng(0, "kv8", "x").standard_normal((T, cfg.qkv_dim)), cfg)
+    some = db.host_runs if db.n_runs < T else db.host_runs[:-1]
+    want = appended(cfg, db, num_pages, cache, x, some)
+    free = np.tile(np.array([[-1, 0]], dtype=np.int32), (T - len(some), 1))
+    behind = np.concatenate((some, free))
+    say("append", cfg.name, reqs_in, "%d runs in %d places" % (len(some), T))
+    for runs in (behind, behind[gen.rng(1, "kv8", "places").permutation(T)]):
+        assert all(torch.equal(a, b) for a, b in zip(appended(cfg, db, num_pages, cache, x, runs), want))
