@@ -56,7 +56,8 @@ int32_t flexco_kv8_runs(const flexco_maps* host_maps, int32_t* runs, int32_t cap
  * A run that begins its page begins the page's scale, and what the page's other slots held is lost; any other run keeps the scale
  * or raises it, and then rounds the codes of all the page's other slots to the new one.
  * Reads of cfg: n_q_heads, n_kv_heads, head_dim, dtype, page_size, rope_theta.
- * Errors: EINVAL, ESHAPE (head_dim no multiple of 16), EPAGE (maps of a larger pool), EHIP. */
+ * Errors: EINVAL, ESHAPE (head_dim no multiple of 16), EPAGE (maps of a larger pool), EUNSUPPORTED (a token's kv heads take more LDS
+ * than a block has, 8 head_dim + n_kv_heads (head_dim + 16) > 49152; more than 2^24 runs x kv heads), EHIP. */
 int32_t flexco_kv8_append(const flexco_layer_cfg* cfg, const flexco_maps* maps, const int32_t* runs, int32_t n_runs,
                           const void* qkv, const flexco_kv8_pool* pool, void* q_out, size_t ld_q, void* stream);
 
@@ -73,12 +74,13 @@ int32_t flexco_kv8_attention(const flexco_layer_cfg* cfg, const flexco_maps* map
  * pages dst_pages of wide (layout of flexco.h); the slots behind them in the last page are written as zeros.  src_pages,
  * dst_pages: device int32 [ceil(n_tokens / page_size)]; a pair with an id outside its pool is left out, no page may be
  * written twice in a call.  The two pools may differ in their number of pages, not in page_size.
- * Errors: EINVAL, ESHAPE, EHIP. */
+ * Errors: EINVAL, ESHAPE, EUNSUPPORTED (more than 2^24 pages x kv heads), EHIP. */
 int32_t flexco_kv8_expand(const flexco_layer_cfg* cfg, const flexco_kv8_pool* pool, const int32_t* src_pages, int32_t n_tokens,
                           const flexco_kv_pool* wide, const int32_t* dst_pages, void* stream);
 
 /* flexco_layer_forward over an 8-bit pool: flexco_kv8_append (of all the batch's runs) and flexco_kv8_attention in place of the 16-bit
- * steps, everything else - arguments, the finetune window's saved rows, workspace - as there.  A later flexco_lora_bwd of the window takes a pool that
+ * steps, everything else - arguments, the finetune window's saved rows, workspace - as there.  What flexco_kv8_append refuses is
+ * refused here, before anything is launched.  A later flexco_lora_bwd of the window takes a pool that
  * flexco_kv8_expand has filled with the sequence's pages. */
 int32_t flexco_kv8_layer_forward(const flexco_layer_cfg* cfg, const flexco_base_weights* w, const flexco_lora* lora,
                                  const flexco_maps* maps, const int32_t* runs, int32_t n_runs, const void* x_in, void* x_out,

@@ -421,6 +421,7 @@ int32_t check_runs(const flexco_layer_cfg& c, const flexco_maps& m, const int32_
   FLEXCO_CHECK(runs != nullptr && ((uintptr_t)runs & 3u) == 0, FLEXCO_EINVAL, "runs is NULL or misaligned");
   FLEXCO_CHECK(n_runs > 0 && n_runs <= m.T, FLEXCO_EINVAL, "%d runs for a batch of %d tokens", n_runs, m.T);
   FLEXCO_CHECK((int64_t)n_runs * c.n_kv_heads <= (1 << 24), FLEXCO_EUNSUPPORTED, "%d runs x %d heads are too many", n_runs, c.n_kv_heads);
+  FLEXCO_CHECK(kv8_append_token_lds(c) <= KV8_APPEND_LDS, FLEXCO_EUNSUPPORTED, "8-bit append: %d kv heads of %d are too many", c.n_kv_heads, c.head_dim);
   return FLEXCO_OK;
 }
 

@@ -5,6 +5,7 @@
 // codes already there on the spot.  Bound by HBM for many tokens: (2 nq + 2 nkv) d activations and 2 nkv d bytes per token (4000 tokens of chunks over
 // 32/8 heads 22.0 us, 4.1 TB/s), by latency for few (one 5.7 us, 512 single ones over 40/8 heads 9.0).
 // Keys are rotated in double precision and rounded once, into the cache (an angle's fp32 error of 5e-7 moved one code in 10^5).
+#include <algorithm>
 #include "flexco_internal.h"
 #include "flexco_kv8.h"
 #include "kv8_codes.h"
@@ -474,7 +475,8 @@ __device__ inline void append_any(const AppendArgs& a, const RopeFreq& freq, con
 // sixteen, head_dim 16 FORM; 1: any.
 template <typename T, int FORM>
 __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeFreq freq, const T* qkv, T* q_out) {
-  extern __shared__ double cs[];              // [tokens][d] angles (pages of sixteen: fp32); then 2 nkv largest magnitudes, as many old scales, nkv d codes
+  // angles [tokens][d] (pages of sixteen: fp32), then largest magnitudes: two, or of a single token 2 nkv with as many old scales and nkv d codes
+  extern __shared__ double cs[];
   const int run = FORM == 0 ? blockIdx.x : blockIdx.x / a.nkv, kvh = FORM == 0 ? 0 : blockIdx.x % a.nkv;
   constexpr int QP = FORM == 0 ? 2 : 0;
   TokenRow<T, QP> held;
@@ -493,7 +495,7 @@ __global__ __launch_bounds__(THREADS) void kv8_append_kernel(AppendArgs a, RopeF
   if (FORM != 0 || t0 != run) sl = a.slot[t0];
   const int page = sl / a.ps, at = sl % a.ps;
   if (sl < 0 || page >= a.num_pages || at + n > a.ps) return;
-  uint32_t* amax = reinterpret_cast<uint32_t*>(cs + (FORM == 0 ? 1 : FORM == 1 ? GROUP : GROUP / 2) * a.d);
+  uint32_t* amax = reinterpret_cast<uint32_t*>(cs + (n == 1 ? 1 : FORM == 1 ? GROUP : GROUP / 2) * a.d);
   if (n == 1) {
     const T* row = row_of(a, qkv, t0);
     if (FORM != 0 || t0 != run) {
@@ -567,9 +569,9 @@ int32_t launch_kv8_append(const flexco_layer_cfg& c, const flexco_maps& m, const
   const bool single_tokens = n_runs == m.T && (m.n_req == m.T || c.page_size == 1);
   const int form = single_tokens ? 0 : c.page_size == 16 && c.head_dim == 128 ? 8 : c.page_size == 16 && c.head_dim == 64 ? 4 : 1;
   const dim3 grid(form == 0 ? (unsigned)n_runs : (unsigned)n_runs * c.n_kv_heads);
-  const size_t shm = sizeof(double) * (form == 0 ? 1 : form == 1 ? GROUP : GROUP / 2) * c.head_dim +
-                     (4 * sizeof(uint32_t) + c.head_dim) * c.n_kv_heads;
-  if (shm > 48 * 1024) return fail(FLEXCO_EUNSUPPORTED, "8-bit append: %d kv heads of %d are too many", c.n_kv_heads, c.head_dim);
+  // (a block holds a single token or a run of several, and either lies where the other would; kv8_append_token_lds is checked by the entry points)
+  const size_t several = form == 0 ? 0 : sizeof(double) * (form == 1 ? GROUP : GROUP / 2) * c.head_dim + 2 * sizeof(uint32_t);
+  const size_t shm = std::max(kv8_append_token_lds(c), several);
 #define FLEXCO_KV8_APPEND(T_, FORM_) \
   hipLaunchKernelGGL((kv8_append_kernel<T_, FORM_>), grid, dim3(THREADS), shm, s, a, freq, (const T_*)qkv, (T_*)q_out)
 #define FLEXCO_KV8_APPEND_FORMS(T_)                  \

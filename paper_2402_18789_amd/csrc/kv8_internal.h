@@ -5,6 +5,12 @@
 
 namespace flexco {
 
+// LDS of the block that takes a single token, all kv heads of it: angles, largest magnitudes and old scales, codes of the values
+constexpr size_t KV8_APPEND_LDS = 48 * 1024;
+inline size_t kv8_append_token_lds(const flexco_layer_cfg& c) {
+  return sizeof(double) * c.head_dim + (size_t)c.n_kv_heads * (4 * sizeof(uint32_t) + c.head_dim);
+}
+
 // q_cache: NULL, or where the finetune window's rotated queries go as well (its first row's)
 int32_t launch_kv8_append(const flexco_layer_cfg& c, const flexco_maps& m, const int32_t* runs, int n_runs, const void* qkv,
                           const flexco_kv8_pool& pool, void* q_out, size_t ld_q, void* q_cache, hipStream_t s);

@@ -86,3 +86,10 @@ def test_runs_with_places_left_free(cfg, reqs_in):
     say("append", cfg.name, reqs_in, "%d runs in %d places" % (len(some), T))
     for runs in (behind, behind[gen.rng(1, "kv8", "places").permutation(T)]):
         assert all(torch.equal(a, b) for a, b in zip(appended(cfg, db, num_pages, cache, x, runs), want))
+
+
+# ---- many kv heads -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cfg", [shape(64, 64, 256), shape(64, 64, 256, "f32")], ids=lambda c: c.name)
+def test_append_of_many_kv_heads(cfg):
+    check_append(cfg, [(D, 33, 1), (P, 5, 20)])
