@@ -11,7 +11,8 @@
  *
  * What flexco_kv8_append writes: the scale of a page is 2^e with e >= -117 the least that keeps its elements within 448 (code x scale
  * is then exact in bf16, and a scale that grows later costs codes no second rounding but below the type's smallest normal
- * number).  Elements that are no finite number are stored as NaN and take no part in a scale.
+ * number).  Elements that are no finite number are stored as NaN and take no part in a scale.  Finite ones beyond 1.875 x 2^127 are stored as
+ * that, off by less than 2^-4: under the largest scale, 2^120, the next number is an infinity in the activations' types.
  */
 #ifndef FLEXCO_KV8_H
 #define FLEXCO_KV8_H

@@ -8,6 +8,7 @@ from . import ops
 MAGNITUDES = np.array([m * 2.0 ** -9 for m in range(8)] + [(1 + m / 8) * 2.0 ** (e - 7) for e in range(1, 16) for m in range(8)])[:127]
 LARGEST = 448.0
 LEAST_EXP = -117
+MOST = 1.875 * 2.0 ** 127        # finite elements beyond it are stored as it is: the next number is 2^128, in bf16 and fp32 infinite
 
 
 def decode(codes):
@@ -54,7 +55,7 @@ class Cache8:
             for name, rows in (("k", k), ("v", v)):
                 new = np.asarray(rows[p - start:p - start + m], dtype=np.float64).reshape(m, self.nkv, self.d)
                 for h in range(self.nkv):
-                    x = new[:, h]
+                    x = np.where(np.isfinite(new[:, h]), np.clip(new[:, h], -MOST, MOST), new[:, h])
                     s = scale_for(np.max(np.abs(x), where=np.isfinite(x), initial=0.0))
                     old = self.scale[name][page, h]
                     codes = self.codes[name][page, :, h]

@@ -85,8 +85,8 @@ struct Angles8 {
     }
   }
 };
-// Largest magnitude of sixteen elements, those that are no finite number left out; all: there was none of these.  (x 0 summed is NaN
-// where one is infinite or NaN: a multiply-add per element instead of two comparisons in the two places that ask.)
+// Largest magnitude of sixteen elements, those that are no finite number left out; all: every one is stored as it is (kv8_storable).  (x 0
+// summed is NaN where one is infinite or NaN: a multiply-add per element instead of two comparisons in the two places that ask.)
 __device__ inline float largest16(const float* v, bool* all) {
   float odd = 0.f, m = 0.f;
 #pragma unroll
@@ -99,6 +99,7 @@ __device__ inline float largest16(const float* v, bool* all) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) m = fmaxf(m, kv8_finite(v[e]) ? fabsf(v[e]) : 0.f);
   }
+  *all = *all && m <= KV8_MOST;
   return m;
 }
 
@@ -131,7 +132,7 @@ __device__ inline u32x2 encode8(const float* v, float inv, bool all) {
   for (int e = 0; e < 8; ++e) w[e] = v[e] * inv;
   if (!all)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = kv8_storable(w[e]);
+    for (int e = 0; e < 8; ++e) w[e] = kv8_storable(v[e]) * inv;
   return u32x2{kv8_encode4(w), kv8_encode4(w + 4)};
 }
 template <typename T>

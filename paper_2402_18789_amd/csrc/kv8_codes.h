@@ -23,8 +23,11 @@ __device__ inline void kv8_decode16(const u32x4& w, float* v) {
 }
 
 __device__ inline bool kv8_finite(float v) { return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) != 0x7f800000u; }
+// Finite numbers beyond this are stored as it is: the largest scale is 2^120, and above 1.9375 2^127 the nearest code times it is 2^128,
+// an infinity in the activations' types (1.875 2^127 is off by less than 2^-4).
+constexpr float KV8_MOST = 0x1.ep127f;
 // what a cached element is stored from: x, or NaN for what is no finite number
-__device__ inline float kv8_storable(float x) { return kv8_finite(x) ? x : __builtin_nanf(""); }
+__device__ inline float kv8_storable(float x) { return kv8_finite(x) ? fminf(fmaxf(x, -KV8_MOST), KV8_MOST) : __builtin_nanf(""); }
 
 // The least 2^e >= 2^-117 with amax <= 448 2^e; amax finite, not negative.  amax = 1.f 2^E; 448 = 1.75 2^8, so e = E - 8, and one
 // more where the fraction is above 1.75.  (Below 2^-117 a code times its scale could be a bf16 subnormal.)

@@ -93,3 +93,61 @@ def test_runs_with_places_left_free(cfg, reqs_in):
 @pytest.mark.parametrize("cfg", [shape(64, 64, 256), shape(64, 64, 256, "f32")], ids=lambda c: c.name)
 def test_append_of_many_kv_heads(cfg):
     check_append(cfg, [(D, 33, 1), (P, 5, 20)])
+
+
+# ---- the top of the number range ----------------------------------------------------------------------------
+
+TOP = [1.0, 1.74, 1.75, 1.76, 1.87, 1.875, 1.9, 1.9374, 1.9376, 1.97, 1.9921875]     # times 2^127
+
+
+@pytest.mark.parametrize("cfg", [shape(), shape(4, 2, 64, "f32"), shape(16, 16, 256), shape(3, 3, 48, "f32"), shape(4, 2, 128, "f32", 5)], ids=lambda c: c.name)
+@pytest.mark.parametrize("reqs_in", [[(D, 0, 1), (D, 33, 1)], [(P, 0, 33), (D, 0, 1), (D, 5, 1)]], ids=str)
+def test_the_largest_numbers_stay_finite(cfg, reqs_in):
+    """Finite rows of up to 1.99 x 2^127 read back as finite numbers off by at most 2^-4 of themselves (half a step of the code, and 1.875 x 2^127,
+    that nothing is stored beyond, is 0.0588 below 1.9922 x 2^127), or, of elements below 2^-6 of the scale, half the smallest code: 2^-10 of it."""
+    reqs, pages, num_pages = make_batch(cfg, reqs_in)
+    cache = O8.Cache8(num_pages, cfg.page_size, cfg.n_kv_heads, cfg.head_dim)
+    fill_prefixes(cfg, cache, reqs, pages, 0)
+    db = kv8.DeviceBatch8(cfg, reqs, pages, num_pages)
+    T, qd, kd, half = db.host_maps.T, cfg.q_dim, cfg.kv_dim, cfg.head_dim // 2
+    g = gen.rng(0, "kv8", "top")
+    x = np.zeros((T, cfg.qkv_dim))
+    big = lambda n: g.choice(TOP, (T, n)) * 2.0 ** 127 * g.choice([-1, 1], (T, n))  # noqa: E731
+    # (of a pair of a key's channels one is zero: what the rotation makes of the other is no larger than it)
+    x[:, qd:qd + kd].reshape(T, cfg.n_kv_heads, 2, half)[:, :, 0] = big(kd // 2).reshape(T, cfg.n_kv_heads, half)
+    x[:, qd + kd:] = big(kd)
+    x = gen.storage_round(cfg, x.astype(np.float32)).astype(np.float64)
+    assert np.isfinite(x).all()
+    xd = device(x, cfg)
+    pool, c = to_device(cfg, cache, num_pages), HH.c_cfg(cfg)
+    q = torch.zeros((T, qd), dtype=xd.dtype, device="cuda")
+    say("append", cfg.name, reqs_in, "at the top of the range")
+    kv8.flexco_kv8_append(c, db.maps, db.runs, db.n_runs, xd, pool.c, q, qd)
+    codes, scale = from_device(pool)
+    pos = np.concatenate([np.arange(r.start_pos, r.start_pos + r.n_new) for r in reqs])
+    from oracle import ops
+    rows = {"k": ops.rope(x[:, qd:qd + kd], pos, cfg.n_kv_heads, cfg.head_dim, cfg.rope_theta), "v": x[:, qd + kd:]}
+    t0 = 0
+    for r in reqs:
+        end = r.start_pos + r.n_new
+        wide = HH.DevicePool(cfg, len(pages[r.seq_id]))
+        seq = torch.arange(len(pages[r.seq_id]), dtype=torch.int32, device="cuda")
+        pool.expand(torch.from_numpy(pages[r.seq_id]).cuda(), end, wide, seq)
+        got = {"k": to_np(wide.k).transpose(0, 2, 1, 3).reshape(-1, kd)[r.start_pos:end],
+               "v": to_np(wide.v).transpose(0, 3, 1, 2).reshape(-1, kd)[r.start_pos:end]}
+        for name in "kv":
+            want = rows[name][t0:t0 + r.n_new]
+            s = np.repeat(scale[name][pages[r.seq_id][np.arange(r.start_pos, end) // cfg.page_size]], cfg.head_dim, 1)
+            assert s.max() <= 2.0 ** 120 and np.isfinite(got[name]).all(), name
+            # (1e-6: the angles' part, as in check_append)
+            assert np.all(np.abs(got[name] - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * s) + 1e-6 * 2.0 ** 128), name
+        t0 += r.n_new
+    # a token alone, with equal scores for all of its one key: its value as it is cached
+    alone = [t for t, r in zip(np.cumsum([0] + [r.n_new for r in reqs]), reqs) if r.start_pos == 0 and r.n_new == 1]
+    ws = HH.Workspace(c, T, db.host_maps.n_parts)
+    out = torch.empty_like(q)
+    kv8.flexco_kv8_attention(c, db.maps, q, pool.c, out, None, ws.ptr, ws.bytes)
+    i = [r for r in reqs if r.start_pos == 0 and r.n_new == 1][0].seq_id
+    cached = O8.decode(codes["v"][pages[i][0], 0]) * scale["v"][pages[i][0]][:, None]
+    want = np.repeat(cached, cfg.n_q_heads // cfg.n_kv_heads, 0).reshape(-1)
+    assert np.all(np.abs(to_np(out)[alone[0]] - want) <= 2.0 ** -22 * np.abs(want))
