@@ -151,3 +151,65 @@ def test_the_largest_numbers_stay_finite(cfg, reqs_in):
     cached = O8.decode(codes["v"][pages[i][0], 0]) * scale["v"][pages[i][0]][:, None]
     want = np.repeat(cached, cfg.n_q_heads // cfg.n_kv_heads, 0).reshape(-1)
     assert np.all(np.abs(to_np(out)[alone[0]] - want) <= 2.0 ** -22 * np.abs(want))
+
+
+# ---- the layer ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("single", [False, True], ids=["mixed", "decode"])
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_rows_that_the_layer_caches(name, single):
+    """every key and value element that flexco_kv8_layer_forward caches, against the definition in 64 bits: within half a code's step, the
+    rotation's error and that of the storage type and the sums, element by element (a quiet head has a bound of its own size).
+
+    With A = sum of |h| |W| (and of the adapter's |h| |A| |B|) of an element: the norm's rows, the adapter's inner rows and the element itself are stored once
+    each, 2^-8 A at most in bf16 (fp32: 2^-24 A); sums of hidden + 64 terms in fp32, those of the norm among them."""
+    cfg = (C2.with_(name="kv8_layer", hidden=512, n_q_heads=8, n_kv_heads=2, ffn=1408) if name == "bf16" else C1)
+    seed = 4
+    batch = gen.batch_scaled(seed, 6, 3, 200, [] if single else [(0, 70, 70), (64, 40, 150)], [] if single else [(96, 50, 146)])
+    W, lora = gen.layer_weights(cfg, seed, 0), gen.lora_weights(cfg, seed, 0)
+    for w in ("wk", "wv"):                                             # the first head a thousandth as loud as the last
+        W[w][:cfg.head_dim] = gen.storage_round(cfg, W[w][:cfg.head_dim] * np.float32(1e-3))
+    dev = HH.DeviceLayer(cfg, W, lora)
+    ft_req = [r for r in batch.requests if r.kind == KIND_FINETUNE]
+    L = batch.seq_capacity[ft_req[0].seq_id] if ft_req else 0
+    cache = O8.Cache8(batch.num_pages, cfg.page_size, cfg.n_kv_heads, cfg.head_dim)
+    pool = to_device(cfg, cache, batch.num_pages)
+    db = kv8.DeviceBatch8(cfg, batch.requests, batch.seq_pages, batch.num_pages)
+    hm = db.host_maps
+    ws = HH.Workspace(dev.c, hm.T, hm.n_parts, ft_req[0].n_new if ft_req else 0, L)
+    x = device(gen.layer_input(cfg, seed, hm.T), cfg)
+    y, ft = torch.empty_like(x), HH.DeviceFtState(cfg, L) if ft_req else None
+    say("layer", cfg.name, hm.T, "tokens")
+    kv8.flexco_kv8_layer_forward(dev.c, dev.w, dev.lora, db.maps, db.runs, db.n_runs, x, y, pool.c, ft.c if ft else None, ws.ptr, ws.bytes)
+    codes, scale = from_device(pool)
+    om = build_maps(batch.requests, batch.seq_pages, batch.page_size, batch.num_pages)
+    states = {ft_req[0].seq_id: OL.FtState(cfg, L)} if ft_req else None
+    want = OL.layer_forward_mixed(cfg, W, lora, om, to_np(x), OL.KVPool(batch.num_pages, cfg.page_size, cfg.kv_dim), states, return_all=True)
+    slot = om["slot"].astype(np.int64)
+    page, at = slot // cfg.page_size, slot % cfg.page_size
+    h = np.abs(want["h1"])
+    step, fp32 = (2.0 ** -8 if name == "bf16" else 2.0 ** -24), 2.0 ** -24 * (cfg.hidden + 64)
+    quiet = 1.0
+    for n in "kv":
+        A = h @ np.abs(W["w" + n]).astype(np.float64).T + (np.abs(W["b" + n]) if "b" + n in W else 0)
+        if n in lora:
+            A += cfg.lora_scale * (h @ np.abs(lora[n][0])) @ np.abs(lora[n][1])
+        err = (3 * step + fp32) * A
+        if n == "k":                                                  # a rotated element has the errors of both of its pair
+            pair = err.reshape(hm.T, cfg.n_kv_heads, 2, -1)
+            err = np.repeat(pair.sum(2, keepdims=True), 2, 2).reshape(hm.T, -1)
+            B = np.abs(want["k"]).reshape(hm.T, cfg.n_kv_heads, 2, -1)
+            err = err + 2e-6 * np.repeat(B.sum(2, keepdims=True), 2, 2).reshape(hm.T, -1)
+        rows = want[n]
+        s = np.repeat(scale[n][page], cfg.head_dim, 1)
+        got = (O8.decode(codes[n][page, at]) * scale[n][page][:, :, None]).reshape(hm.T, -1)
+        assert np.all(np.abs(got - rows) <= half_step(np.abs(rows) + err, s) + err), n
+        # the scale is that of the page's own elements, and not of something larger
+        most = np.zeros((batch.num_pages, cfg.n_kv_heads))
+        np.maximum.at(most, page, (np.abs(rows) + err).reshape(hm.T, cfg.n_kv_heads, -1).max(2))
+        for p in np.unique(page):
+            for j in range(cfg.n_kv_heads):
+                assert 0 < scale[n][p, j] <= O8.scale_for(most[p, j]), (n, p, j)
+        by_head = np.abs(rows).reshape(hm.T, cfg.n_kv_heads, -1).mean((0, 2))
+        quiet = min(quiet, by_head[0] / by_head[-1])
+    assert quiet < 0.5
