@@ -10,7 +10,9 @@
 // they drop what lies 2^-13 below the largest product of a sum, and scores came out 1e-5 off.)
 // A lane (col = lane % 16, g = lane / 16) gets keys 4 g .. 4 g + 3 of each page from the first product and supplies page g's sixteen
 // keys of four pages to the second: eight words change places between the rows of lanes, by swaps of halves and of pairs.
-// Scores, running maxima and sums, and the products' sums are fp32; probabilities are rounded to bf16 for the second product.
+// Scores, running maxima and sums, and the products' sums are fp32.  Probabilities are rounded to bf16 for the second product, as the 16-bit cache's
+// are, and summed unrounded: a row is off by 2^-8 of its sum of p |v| at most, on the order of the output's storage (outputs 0.0020 - 0.0022 from
+// 64 bits, relative to their norm, the storage alone 0.0016 - 0.0017).  Two bf16 terms of each would double that product's instructions.
 //
 // Key positions behind a column's own are masked in the scores, and what lies in V at such positions never meets the sums: slots
 // behind the item's last position are cleared, and a NaN code between (a later token of the same chunk) is taken out and
@@ -306,9 +308,9 @@ __device__ inline void token_block(const Args& a, const Tables& tab, const Token
 }
 
 // ---- chunks --------------------------------------------------------------------------------------------------
-// Bound by the card's power where launches follow each other, by vector instructions beside the products (conversions and
-// exponentials) in a launch of its own: 4096 new tokens over 40/8 heads (171 GFLOP) 200 - 216 us on several cards, 177 with codes and
-// queries of zeros.  Each of the block's two wavefronts takes two tiles as 32 columns; the pages of a step lie once in LDS for
+// Bound by vector instructions beside the products (conversions and exponentials: issued on 57 % of the cycles, matrix pipes busy on 39 %), and
+// by the card's power where launches follow each other: 4096 new tokens over 40/8 heads (171 GFLOP, 142 us at a large product's rate)
+// 200 - 216 us on several cards, 177 with codes and queries of zeros.  Each of the block's two wavefronts takes two tiles as 32 columns; the pages of a step lie once in LDS for
 // both, as they lie in memory, and the next step's are on their way meanwhile.  v_mfma_f32_32x32x16_bf16:
 //   S^T[key, col]: A = two K pages, lane (r = lane % 32, h = lane / 32): channels 32 i + 16 h .. + 15, two products' worth, of the key in
 //                  slot (r with bits 2 and 3 exchanged) % 16 of page r / 16

@@ -3,7 +3,8 @@
 // Append.  A page's scale is chosen from all of its new rows, so the rotated keys and the values of a (run, kv head) are held until
 // their largest magnitude is known; whoever does that owns the page's codes of the head, so a scale that has grown is applied to the
 // codes already there on the spot.  Bound by HBM for many tokens: (2 nq + 2 nkv) d activations and 2 nkv d bytes per token (4000 tokens of chunks over
-// 32/8 heads 22.0 us, 4.1 TB/s), by latency for few (one 5.7 us, 512 single ones over 40/8 heads 9.0).
+// 32/8 heads 22.5 us, 4.0 TB/s), by latency for few (one 5.8 us, 512 single ones over 40/8 heads 9.1, where all of them raise their pages'
+// scales about 15).
 // Keys are rotated in double precision and rounded once, into the cache (an angle's fp32 error of 5e-7 moved one code in 10^5).
 #include <algorithm>
 #include "flexco_internal.h"
